@@ -76,7 +76,9 @@ typedef enum {
   ATTN_ERR_SCALE = -6,      /* softmax_scale not finite or <= 0 */
   ATTN_ERR_WORKSPACE = -7,  /* workspace NULL, misaligned (256 B) or too small */
   ATTN_ERR_MASK = -8,       /* mask_block != 128 or negative mask stride */
-  ATTN_ERR_LAUNCH = -9      /* the HIP runtime refused the launch */
+  ATTN_ERR_LAUNCH = -9,     /* the HIP runtime refused the launch */
+  ATTN_ERR_PAGES = -10,     /* page size no power of two in [16, 4096], or a list of page copies that names a page it must not */
+  ATTN_ERR_ROTARY = -11     /* rotary_dim odd or not in [2, d], no frequencies, or a factor that is not finite */
 } attn_status;
 
 enum { ATTN_FP16 = 0, ATTN_BF16 = 1 };
@@ -276,6 +278,116 @@ int attn_debug_bwd_kernel(const attn_params* p, size_t workspace_bytes, int32_t*
  * -1 leaves a setting unchanged.  Process-wide and thread-safe; affects calls issued afterwards.
  */
 int attn_debug_set_variant(int32_t fwd_variant, int32_t dkv_variant);
+
+/*
+ * ---- Rotary positions and the paged key/value cache ----
+ *
+ * What a program with attention over a growing context calls around it.  The conventions above hold: device
+ * pointers of the caller, the caller's stream, all argument checks on the host, nothing allocated or kept.  The device of the
+ * tensors must be the current one.
+ */
+
+/* Which columns of a row turn, and how fast. */
+typedef struct {
+  const double* frequencies;  /* device, [rotary_dim / 2]: radians a position                              */
+  int32_t rotary_dim;         /* r: the first r columns turn (even, 2 <= r <= d), the others are copied      */
+  int32_t interleaved;        /* != 0: pair i is columns (2 i, 2 i + 1); 0: columns (i, i + r / 2)           */
+  float magnitude;            /* m: factor of the turned columns                                           */
+} attn_rotary_spec;
+
+/* A [B,H,N,d] tensor and where its turned copy goes (y == x with the same strides: in place).  Strides in elements, multiples of 8, the d axis
+ * contiguous; pointers 16-byte aligned.  x and y must not overlap otherwise. */
+typedef struct {
+  const void* x;
+  void* y;
+  int32_t H;
+  int64_t x_stride_b, x_stride_h, x_stride_n;
+  int64_t y_stride_b, y_stride_h, y_stride_n;
+} attn_rotary_tensor;
+
+typedef struct {
+  int32_t B, N, d;             /* d in {16, 32, 64, 128} */
+  int32_t dtype;
+  attn_rotary_spec rotary;
+  int32_t inverse;             /* != 0: by the negative angle (the gradient of the rotation) */
+  const int32_t* positions;    /* device, [N] or [B, N]; NULL: 0 .. N - 1.  Any int32 value */
+  int64_t position_stride_b;   /* elements from one batch entry to the next (0: all share one row) */
+  void* stream;
+} attn_rotary_params;
+
+/*
+ * Pair i of a row at position p turns by the angle p f_i:  y_a = m (x_a cos - x_b sin),  y_b = m (x_b cos + x_a sin).
+ * One or two tensors (Q and K, which may differ in their number of heads) in one launch.  The angle is formed in
+ * 64 bits and reduced to a turn before it is rounded: every int32 position is as exact as a near one.
+ */
+int attn_rotary(const attn_rotary_params* p, const attn_rotary_tensor* tensors, int32_t n_tensors);
+
+/*
+ * A batch of B sequences whose keys and values lie in the pages of a cache.
+ *   caches         K and V: [pages, Hk, page_size, d], strides shared by both (multiples of 8 elements, d contiguous)
+ *   block_table    device int32 [B, table_width]: entry t of row b is the page of positions t * page_size ...
+ *   lengths        device int32 [B]: tokens of each sequence, the new ones included
+ *   query_starts   device int32 [B + 1], rising: rows query_starts[b] .. query_starts[b + 1] - 1 of the token tensors [T, heads, d] are the
+ *                  new tokens of sequence b, its last ones.  NULL: row b is the one new token of sequence b (then T >= B).
+ *                  Rows of no sequence (behind the last, in a padded batch) are not read, and are left as they were in the outputs.
+ * These three are read on the GPU only: a captured graph follows their contents.  Whatever they hold, nothing outside the tensors is
+ * read or written: lengths are taken as at most table_width * page_size, starts as at most T, and a page
+ * number outside [0, pages) stands for a page of zeros that nothing is written to.  (Table entries behind a sequence's length are not used.)
+ * What stands in the pages at positions < length must be finite; what stands behind is never used.
+ */
+typedef struct {
+  int32_t B, T;
+  int32_t Hq, Hk, d;           /* Hq a multiple of Hk: Q head h reads K head h / (Hq / Hk); d in {16, 32, 64, 128} */
+  int32_t dtype;
+  int32_t pages, page_size, table_width;   /* page_size: a power of two from 16 to 4096 */
+  int32_t causal;              /* != 0: a new token sees its own position and those before it; 0: all positions < length */
+  float softmax_scale;
+  int64_t page_stride, head_stride, row_stride;   /* of the caches */
+  int64_t table_stride;        /* elements between rows of the block table */
+  int64_t q_stride_t, q_stride_h;      /* Q [T, Hq, d] */
+  int64_t o_stride_t, o_stride_h;      /* O (attn_paged_append: the turned Q) */
+  int64_t k_stride_t, k_stride_h, v_stride_t, v_stride_h;   /* new K and V [T, Hk, d] (attn_paged_append only) */
+  const int32_t* block_table;
+  const int32_t* lengths;
+  const int32_t* query_starts;
+  void* stream;
+} attn_paged_params;
+
+/*
+ * Writes the new tokens' K and V rows into the pages, token i of the m new ones of sequence b at position lengths[b] - m + i (a position that is negative, or behind
+ * the table's last page, is not written).  With rotary != NULL K is turned by its position, and so is Q, if one is given, into Qout (in place where
+ * Qout == Q with the same strides).  rotary == NULL: K is copied; then Q must be NULL.
+ */
+int attn_paged_append(const attn_paged_params* p, const attn_rotary_spec* rotary, const void* K, const void* V, void* k_cache, void* v_cache, const void* Q,
+                      void* Qout);
+
+/* Bytes of scratch for attn_paged_fwd with these params (B, T, Hq, Hk, d decide).  0 if the params are invalid. */
+size_t attn_paged_workspace_bytes(const attn_paged_params* p);
+
+/*
+ * O = softmax(tau Q K^T) V and its row statistic for the new tokens of every sequence over its pages.
+ *   Q, O       [T, Hq, d] with strides of their own;   LSE  [Hq, T] float32, packed
+ *   workspace  256-byte aligned, attn_paged_workspace_bytes(p); contents on entry are ignored, and calls that overlap in time must not share one
+ * A row that sees no key (a sequence of length 0, a token whose position is negative) gets O = 0, LSE = -inf.  Results do not depend on timing: for the
+ * same sizes and lengths they are the same in every call.
+ */
+int attn_paged_fwd(const attn_paged_params* p, const void* Q, const void* k_cache, const void* v_cache, void* O, float* LSE, void* workspace,
+                   size_t workspace_bytes);
+
+/* Caches of one or more layers, [layers, pages, Hk, page_size, d]. */
+typedef struct {
+  int32_t layers, pages, Hk, page_size, d;
+  int32_t dtype;
+  int64_t layer_stride, page_stride, head_stride, row_stride;
+  void* stream;
+} attn_paged_copy_params;
+
+/*
+ * Copies whole pages, K and V, in all layers.  pairs: HOST memory, [n_pairs][2] (source, destination), read during the call.  All copies are
+ * independent of their order: a page that is the destination of one copy and the source or the destination of another is
+ * refused (ATTN_ERR_PAGES), as is a number outside [0, pages).  A source may be named any number of times.
+ */
+int attn_paged_copy(const attn_paged_copy_params* p, void* k_cache, void* v_cache, const int32_t* pairs, int64_t n_pairs);
 
 /* Static, human-readable text for a status code. */
 const char* attn_strerror(int status);

@@ -15,6 +15,7 @@ import torch
 from torch.autograd import forward_ad
 
 from . import binding
+from .rotary import Rotary
 
 
 class _FlashAttention(torch.autograd.Function):
@@ -44,17 +45,53 @@ class _FlashAttention(torch.autograd.Function):
         return dq, dk, dv, None, None, None, None, None, None, None
 
 
+class _RotaryEmbedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, frequencies, interleaved, magnitude, positions, inverse):
+        ctx.save_for_backward(frequencies, positions)
+        ctx.kw = (interleaved, magnitude, inverse)
+        return binding.attn_rotary(q, k, Rotary(frequencies, interleaved=interleaved, magnitude=magnitude), positions=positions, inverse=inverse)
+
+    @staticmethod
+    def backward(ctx, d_q, d_k):
+        frequencies, positions = ctx.saved_tensors
+        interleaved, magnitude, inverse = ctx.kw
+        return (*_RotaryEmbedding.apply(d_q.contiguous(), d_k.contiguous(), frequencies, interleaved, magnitude, positions, not inverse), None, None, None, None, None)
+
+
+def _node_in_python() -> bool:
+    # The nodes in Python stay for what has rules of its own for functions written in Python: functorch's transforms, forward-mode
+    # differentiation, tracing and compilation.
+    return (torch.compiler.is_compiling() or torch._C._are_functorch_transforms_active() or forward_ad._current_level >= 0
+            or torch.jit.is_tracing())
+
+
+def rotary_embedding(q: torch.Tensor, k: torch.Tensor, rotary: Rotary, positions: Optional[torch.Tensor] = None):
+    """(q', k'): q and k turned by their tokens' positions, differentiable with respect to both (any number of times).
+
+    q, k: [B,H,N,d] fp16 or bf16 CUDA tensors, d contiguous, d in {16, 32, 64, 128}; their numbers of heads and strides may differ.  positions:
+    int32 [N] or [B,N] (default 0 .. N - 1).  One launch forward, one backward.
+    """
+    if binding._lib is None:
+        binding.load()
+    if _node_in_python():
+        return _RotaryEmbedding.apply(q, k, rotary.frequencies, rotary.interleaved, rotary.magnitude, positions, False)
+    return binding._marshal.rotary_embedding(q, k, rotary.frequencies, rotary.interleaved, rotary.magnitude, positions)
+
+
 def flash_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, softmax_scale: Optional[float] = None,
                     causal: bool = False, dropout_p: float = 0.0, seed: Optional[int] = None, offset: int = 0,
                     key_lengths: Optional[torch.Tensor] = None,
-                    block_mask: Optional[torch.Tensor] = None) -> torch.Tensor:
+                    block_mask: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
+                    positions: Optional[torch.Tensor] = None) -> torch.Tensor:
     """softmax(scale * q k^T + mask) v with dropout on the probabilities; exact attention.
 
     q, k, v: [B,H,N,d] fp16 or bf16 CUDA tensors with identical shape and strides, d contiguous,
     d in {16, 32, 64, 128}.  softmax_scale defaults to 1/sqrt(d).  key_lengths: int32 [B] true lengths
     (key-padding mask).  block_mask: uint8 [T,T] or [H,T,T] over 128 x 128 blocks (then N % 128 == 0).
     With dropout_p > 0 the mask is a pure function of (seed, offset, b, h, i, j); seed defaults to a
-    draw from torch's CPU generator, so torch.manual_seed makes a run reproducible.
+    draw from torch's CPU generator, so torch.manual_seed makes a run reproducible.  With `rotary`, q and k are
+    turned by their `positions` first (`rotary_embedding`).
     """
     if not (q.is_cuda and k.is_cuda and v.is_cuda):
         raise RuntimeError("flash_attention runs on the GPU only: there is no CPU path")
@@ -64,10 +101,11 @@ def flash_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, softma
         seed = int(torch.randint(0, 2 ** 62, (), dtype=torch.int64).item())
     if binding._lib is None:
         binding.load()
-    # The node in Python stays for what has rules of its own for functions written in Python: functorch's transforms, forward-mode
-    # differentiation, tracing and compilation.
-    if (torch.compiler.is_compiling() or torch._C._are_functorch_transforms_active() or forward_ad._current_level >= 0
-            or torch.jit.is_tracing()):
+    if rotary is not None:
+        q, k = rotary_embedding(q, k, rotary, positions)
+    elif positions is not None:
+        raise ValueError("positions are of no use without rotary")
+    if _node_in_python():
         apply = _FlashAttention.apply
     else:
         apply = binding._marshal.attention

@@ -23,7 +23,7 @@ ATTN_FP16, ATTN_BF16 = 0, 1
 SYMBOLS = (
     "attn_fwd", "attn_bwd_workspace_bytes", "attn_blocksparse_bwd_workspace_bytes", "attn_bwd", "attn_bwd_static", "attn_blocksparse_fwd",
     "attn_blocksparse_bwd", "attn_bwd_timed", "attn_debug_dropout_mask", "attn_debug_mfma_rate", "attn_debug_kernel_choice", "attn_debug_bwd_kernel", "attn_debug_set_variant", "attn_strerror",
-    "attn_version",
+    "attn_version", "attn_rotary", "attn_paged_append", "attn_paged_workspace_bytes", "attn_paged_fwd", "attn_paged_copy",
 )
 
 
@@ -40,6 +40,35 @@ class AttnParams(ctypes.Structure):
         ("stream", ctypes.c_void_p),
         ("key_lengths", ctypes.c_void_p),
     ]
+
+
+class RotarySpec(ctypes.Structure):
+    _fields_ = [("frequencies", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float)]
+
+
+class RotaryTensor(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("H", ctypes.c_int32),
+                *[(f"{t}_stride_{a}", ctypes.c_int64) for t in "xy" for a in "bhn"]]
+
+
+class RotaryParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("N", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rotary", RotarySpec),
+                ("inverse", ctypes.c_int32), ("positions", ctypes.c_void_p), ("position_stride_b", ctypes.c_int64), ("stream", ctypes.c_void_p)]
+
+
+class PagedParams(ctypes.Structure):
+    _fields_ = [
+        *[(n, ctypes.c_int32) for n in ("B", "T", "Hq", "Hk", "d", "dtype", "pages", "page_size", "table_width", "causal")],
+        ("softmax_scale", ctypes.c_float),
+        *[(n, ctypes.c_int64) for n in ("page_stride", "head_stride", "row_stride", "table_stride", "q_stride_t", "q_stride_h", "o_stride_t", "o_stride_h",
+                                        "k_stride_t", "k_stride_h", "v_stride_t", "v_stride_h")],
+        *[(n, ctypes.c_void_p) for n in ("block_table", "lengths", "query_starts", "stream")],
+    ]
+
+
+class PagedCopyParams(ctypes.Structure):
+    _fields_ = [*[(n, ctypes.c_int32) for n in ("layers", "pages", "Hk", "page_size", "d", "dtype")],
+                *[(n, ctypes.c_int64) for n in ("layer_stride", "page_stride", "head_stride", "row_stride")], ("stream", ctypes.c_void_p)]
 
 
 class AttnError(RuntimeError):
@@ -65,6 +94,12 @@ def _attach(lib: ctypes.CDLL) -> None:
     _marshal.attach(AttnError, *(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
         "attn_fwd", "attn_bwd", "attn_bwd_workspace_bytes", "attn_blocksparse_fwd", "attn_blocksparse_bwd",
         "attn_blocksparse_bwd_workspace_bytes")))
+
+
+def _attach_paged(lib: ctypes.CDLL) -> None:
+    """The same for the rotary positions and the paged cache."""
+    _marshal.attach_paged(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
+        "attn_rotary", "attn_paged_append", "attn_paged_workspace_bytes", "attn_paged_fwd", "attn_paged_copy")))
 
 
 def load() -> ctypes.CDLL:
@@ -105,11 +140,22 @@ def load() -> ctypes.CDLL:
     lib.attn_debug_mfma_rate.restype = ctypes.c_int
     lib.attn_debug_set_variant.argtypes = [i32, i32]
     lib.attn_debug_set_variant.restype = ctypes.c_int
+    lib.attn_rotary.argtypes = [ctypes.POINTER(RotaryParams), ctypes.POINTER(RotaryTensor), i32]
+    lib.attn_rotary.restype = ctypes.c_int
+    lib.attn_paged_append.argtypes = [ctypes.POINTER(PagedParams), ctypes.POINTER(RotarySpec)] + [vp] * 6
+    lib.attn_paged_append.restype = ctypes.c_int
+    lib.attn_paged_workspace_bytes.argtypes = [ctypes.POINTER(PagedParams)]
+    lib.attn_paged_workspace_bytes.restype = sz
+    lib.attn_paged_fwd.argtypes = [ctypes.POINTER(PagedParams)] + [vp] * 5 + [vp, sz]
+    lib.attn_paged_fwd.restype = ctypes.c_int
+    lib.attn_paged_copy.argtypes = [ctypes.POINTER(PagedCopyParams), vp, vp, vp, i64]
+    lib.attn_paged_copy.restype = ctypes.c_int
     lib.attn_strerror.argtypes = [ctypes.c_int]
     lib.attn_strerror.restype = ctypes.c_char_p
     lib.attn_version.argtypes = []
     lib.attn_version.restype = ctypes.c_int
     _attach(lib)
+    _attach_paged(lib)
     _lib = lib
     return lib
 
@@ -267,6 +313,65 @@ def attn_bwd_timed(Q, K, V, O, dO, LSE, events, *, softmax_scale, block_mask=Non
                                  _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(workspace), nbytes, ev),
            "attn_bwd_timed")
     return dQ, dK, dV
+
+
+def attn_rotary(Q, K, rotary, *, positions=None, inverse=False, out=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Q and K (or Q alone: K = None) turned by their positions, [B,H,N,d] each, in one launch; the two may differ in their number of heads.
+
+    rotary: a `rotary.Rotary`.  positions: int32 [N] or [B,N] (None: 0 .. N - 1).  inverse: by the negative angle (the gradient).
+    out: (Q', K'), which may be Q and K themselves; made with the strides of Q and K unless given.  Runs on torch's current stream."""
+    if _lib is None:
+        load()
+    q_out, k_out = (None, None) if out is None else out
+    return _marshal.rotary(Q, K, rotary.frequencies, rotary.interleaved, rotary.magnitude, positions, inverse, q_out, k_out)
+
+
+def attn_paged_append(K, V, k_cache, v_cache, block_table, lengths, query_starts=None, *, Q=None, rotary=None, out=None) -> Optional[torch.Tensor]:
+    """Writes the new tokens' K and V rows [T,Hk,d] into the pages of the caches [pages,Hk,page_size,d], and returns the turned Q [T,Hq,d] if Q is given.
+
+    block_table int32 [B,table_width]: the pages of each sequence in order.  lengths int32 [B]: its tokens, the new ones included.  query_starts int32 [B+1]: rows
+    query_starts[b] .. query_starts[b+1] - 1 are the new tokens of sequence b; None: row b is the one new token of sequence b.  The caches may be views of
+    another order of axes; K and V caches share shape and strides.  rotary: K (and Q, into `out`, which may be Q) are turned by their positions.
+    Rows of no sequence are left as they were (unspecified where `out` is made here).  Runs on torch's current stream."""
+    if _lib is None:
+        load()
+    f, i, m = (None, False, 1.0) if rotary is None else (rotary.frequencies, rotary.interleaved, rotary.magnitude)
+    return _marshal.paged_append(K, V, k_cache, v_cache, block_table, lengths, query_starts, Q, f, i, m, out)
+
+
+def attn_paged_workspace(Q, k_cache, sequences: int) -> torch.Tensor:
+    """A workspace for attn_paged_fwd with these sizes, on the device of Q.  Calls that may overlap in time (other streams, captured graphs that are replayed side by
+    side) need one each.  One made for more than 32 rows (tokens times the Q heads of a K head) a sequence serves fewer rows, too, at the same head dimension."""
+    if _lib is None:
+        load()
+    n = _marshal.paged_workspace_bytes(Q, k_cache, sequences)
+    if n == 0:
+        raise ValueError("attn_paged_fwd does not take these sizes")
+    return torch.empty(n, dtype=torch.uint8, device=Q.device)
+
+
+def attn_paged_fwd(Q, k_cache, v_cache, block_table, lengths, query_starts=None, *, softmax_scale, causal=True, out=None, lse=None,
+                   workspace=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """O [T,Hq,d], LSE [Hq,T]: attention of the new tokens of every sequence over its pages, the new tokens (see attn_paged_append) among them.
+
+    The arguments are those of attn_paged_append; Hq is a multiple of Hk.  causal: a token sees its own position and those before it, else all of its
+    sequence.  A row that sees no key gets O = 0, LSE = -inf.  Outputs and workspace are allocated with torch unless given; rows of no sequence
+    are left as they were (unspecified where the output is made here).  Runs on torch's current stream."""
+    if _lib is None:
+        load()
+    return _marshal.paged_fwd(Q, k_cache, v_cache, block_table, lengths, query_starts, softmax_scale, causal, out, lse, workspace)
+
+
+def attn_paged_copy(k_cache, v_cache, pairs) -> None:
+    """Copies whole pages, K and V: [pages,Hk,page_size,d], or [layers,pages,Hk,page_size,d] with every layer copied.
+
+    pairs: int32 [n,2] on the CPU, or a list of (source, destination).  No destination may be named again, as a source or a destination.  Runs on torch's current stream;
+    a captured graph keeps the list as it was."""
+    if _lib is None:
+        load()
+    if not isinstance(pairs, torch.Tensor):
+        pairs = torch.tensor(pairs, dtype=torch.int32).reshape(-1, 2)
+    _marshal.paged_copy(k_cache, v_cache, pairs)
 
 
 def attn_debug_dropout_mask(B, H, N, dropout_p, seed, offset, device="cuda") -> torch.Tensor:

@@ -388,6 +388,8 @@ const char* attn_strerror(int status) {
     case ATTN_ERR_WORKSPACE: return "workspace is NULL, not 256-byte aligned, or too small (attn_bwd_static: problem beyond the built-in scratch)";
     case ATTN_ERR_MASK: return "mask_block must be 128 and mask_stride_h 0 or >= T*T";
     case ATTN_ERR_LAUNCH: return "kernel launch failed";
+    case ATTN_ERR_PAGES: return "page_size must be a power of two from 16 to 4096; page copies must name pages of the cache, none the destination of one copy and part of another";
+    case ATTN_ERR_ROTARY: return "rotary_dim must be even and in [2, d], with frequencies and a finite magnitude (attn_paged_append: Q only with a rotation)";
     default: return "unknown status";
   }
 }

@@ -11,21 +11,16 @@
 // and more of either are the engine's own change of threads: so much takes the backward of a single product).
 // The functions take positional arguments only (binding.py holds the public signatures and
 // defaults) and raise what the Python marshalling of the measurement entry points raises: ValueError, TypeError, AttnError.
-#define PY_SSIZE_T_CLEAN
-#include <Python.h>
-
-#include <ATen/ATen.h>
-#include <c10/hip/HIPStream.h>
-#include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/custom_function.h>
-#include <torch/csrc/autograd/python_variable.h>
+#include "attn_marshal.h"
 
 #include <algorithm>
-#include <initializer_list>
+#include <vector>
 
-#include "../../include/attn.h"
+PyObject* marshal::attn_error = nullptr;
 
 namespace {
+
+using namespace marshal;
 
 // Entry points of the library that binding.load() opened.
 struct Library {
@@ -37,58 +32,6 @@ struct Library {
   decltype(&attn_blocksparse_bwd_workspace_bytes) sparse_workspace_bytes = nullptr;
 };
 Library lib;
-PyObject* attn_error = nullptr;   // binding.AttnError
-
-struct Raised {};   // a Python error is set
-
-[[noreturn]] void raise(PyObject* type, const char* text) {
-  PyErr_SetString(type, text);
-  throw Raised();
-}
-
-void check_status(int status, const char* where) {
-  if (status == ATTN_OK) return;
-  PyObject* e = PyObject_CallFunction(attn_error, "is", status, where);
-  if (e != nullptr) {
-    PyErr_SetObject(attn_error, e);
-    Py_DECREF(e);
-  }
-  throw Raised();
-}
-
-const at::Tensor& tensor(PyObject* o) {
-  if (!THPVariable_Check(o)) raise(PyExc_TypeError, "expected a torch.Tensor");
-  return THPVariable_Unpack(o);
-}
-void* data(PyObject* o) {   // of a buffer the library checks for: None is its NULL
-  return o == Py_None ? nullptr : tensor(o).data_ptr();
-}
-PyObject* wrap(const at::Tensor& t) {
-  PyObject* o = THPVariable_Wrap(t);
-  if (o == nullptr) throw Raised();
-  return o;
-}
-double number(PyObject* o) {   // float(o)
-  PyObject* f = PyNumber_Float(o);
-  if (f == nullptr) throw Raised();
-  const double v = PyFloat_AS_DOUBLE(f);
-  Py_DECREF(f);
-  return v;
-}
-bool truth(PyObject* o) {
-  const int v = PyObject_IsTrue(o);
-  if (v < 0) throw Raised();
-  return v != 0;
-}
-uint64_t low64(PyObject* o) {   // int(o) & (2^64 - 1)
-  PyObject* i = PyNumber_Long(o);
-  if (i == nullptr) throw Raised();
-  const uint64_t v = PyLong_AsUnsignedLongLongMask(i);
-  Py_DECREF(i);
-  if (v == (uint64_t)-1 && PyErr_Occurred()) throw Raised();
-  return v;
-}
-
 bool alike(const at::Tensor& ref, const at::Tensor& t) {
   return t.sizes() == ref.sizes() && t.strides() == ref.strides() && t.device() == ref.device();
 }
@@ -152,34 +95,8 @@ at::Tensor like(const at::Tensor& q, at::ScalarType type) {
   return at::empty_strided(q.sizes(), q.strides(), q.options().dtype(type));
 }
 
-// The library call itself runs without the interpreter lock.
-template <typename F> int without_gil(F&& f) {
-  PyThreadState* s = PyEval_SaveThread();
-  const int status = f();
-  PyEval_RestoreThread(s);
-  return status;
-}
-
 void expect_args(Py_ssize_t n, Py_ssize_t want) {
   if (n != want || lib.fwd == nullptr) raise(PyExc_TypeError, "internal call with the wrong arguments, or before attach()");
-}
-
-template <typename F> PyObject* guarded(F&& f) {
-  HANDLE_TH_ERRORS
-  try {
-    return f();
-  } catch (const Raised&) {
-    return nullptr;
-  }
-  END_HANDLE_TH_ERRORS
-}
-
-PyObject* tuple(std::initializer_list<PyObject*> items) {   // takes the references over
-  PyObject* t = PyTuple_New((Py_ssize_t)items.size());
-  if (t == nullptr) throw Raised();
-  Py_ssize_t i = 0;
-  for (PyObject* o : items) PyTuple_SET_ITEM(t, i++, o);
-  return t;
 }
 
 // ---- autograd: the forward call keeps what the backward one needs (the O(N) state: O, the row statistic and the generator state)
@@ -198,19 +115,6 @@ attn_params on_current_stream(const Attention& a, const at::Tensor& q) {
   return p;
 }
 int64_t mask_stride(const at::Tensor& mask) { return mask.dim() == 3 ? mask.stride(0) : 0; }
-
-// An error on the engine's thread, which runs without the interpreter lock: `set` raises it, and it is carried to the caller of backward().
-template <typename F> [[noreturn]] void refused_in_backward(F&& set) {
-  const PyGILState_STATE gil = PyGILState_Ensure();
-  python_error e;
-  try {
-    set();
-  } catch (const Raised&) {
-    e.persist();
-  }
-  PyGILState_Release(gil);
-  throw e;
-}
 
 // What the marshalling of a backward call asks of its tensors (backward() below, make_params), of the saved ones as they come back: hooks
 // of the program may have moved, converted or laid out anew some of them, or have given them another batch than the lengths and the masks are for.
@@ -404,16 +308,24 @@ PyObject* py_attach(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-PyMethodDef methods[] = {
+const PyMethodDef own_methods[] = {
     {"attach", (PyCFunction)(void*)py_attach, METH_FASTCALL, nullptr},
     {"attention", (PyCFunction)(void*)py_attention, METH_FASTCALL, nullptr},
     {"fwd", (PyCFunction)(void*)py_fwd, METH_FASTCALL, nullptr},
     {"bwd", (PyCFunction)(void*)py_bwd, METH_FASTCALL, nullptr},
     {"blocksparse_fwd", (PyCFunction)(void*)py_sparse_fwd, METH_FASTCALL, nullptr},
-    {"blocksparse_bwd", (PyCFunction)(void*)py_sparse_bwd, METH_FASTCALL, nullptr},
-    {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+    {"blocksparse_bwd", (PyCFunction)(void*)py_sparse_bwd, METH_FASTCALL, nullptr}};
+std::vector<PyMethodDef> methods;   // of both sources
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, nullptr, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__marshal(void) {
+  methods.assign(std::begin(own_methods), std::end(own_methods));
+  for (const PyMethodDef* m = paged_methods;; ++m) {
+    methods.push_back(*m);
+    if (m->ml_name == nullptr) break;
+  }
+  module.m_methods = methods.data();
+  return PyModule_Create(&module);
+}

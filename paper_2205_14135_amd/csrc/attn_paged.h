@@ -1,0 +1,90 @@
+// Internal declarations of the operators over a paged key/value cache and of the rotary positions: the kernels' arguments and the launchers.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/attn.h"
+#include "attn_common.h"
+
+namespace attn {
+
+// The frequencies and how they pair the columns (attn_rotary_spec, checked).
+struct RotaryArgs {
+  const double* freq;   // [r / 2] radians a position, nullptr: nothing turns (r = 0)
+  int r;                // columns that turn
+  int interleaved;
+  int inverse;
+  float magnitude;
+};
+
+// One [B,H,N,d] tensor of a rotary call.
+struct RotaryTensor {
+  const void* x;
+  void* y;
+  int H;
+  int64_t xb, xh, xn, yb, yh, yn;
+};
+
+struct RotaryCall {
+  RotaryTensor t[2];
+  int n_tensors;
+  int B, N, d;
+  RotaryArgs rot;
+  const int* positions;   // nullptr: 0 .. N - 1
+  int64_t position_sb;
+};
+
+// The sequences of a batch and their pages; see attn_paged_params.
+struct PagedBatch {
+  const int* table;
+  const int* lengths;
+  const int* starts;      // nullptr: token b is the one new token of sequence b
+  int64_t table_stride;
+  int B, T;
+  int Hq, Hk;
+  int pages, page_log2, width;
+  int capacity;           // width << page_log2: tokens that a row of the table holds
+  int64_t sp, sh, sn;     // strides of the caches: page, head, row
+};
+
+struct AppendCall {
+  PagedBatch b;
+  RotaryArgs rot;
+  int d;
+  const void* K; const void* V; const void* Q;
+  void* Kc; void* Vc; void* Qo;
+  int64_t kt, kh, vt, vh, qt, qh, ot, oh;
+};
+
+struct PagedCall {
+  PagedBatch b;
+  const void* Q; const void* K; const void* V;
+  void* O;
+  float* LSE;
+  float* part;            // pieces of divided items
+  int64_t qt, qh, ot, oh;
+  int G;                  // Q heads to a K head
+  int d;                  // of the tensors: 16 runs on the D = 32 kernels
+  int causal;
+  int slots;              // workgroups that share the work
+  float scale_log2;       // tau * log2(e)
+};
+
+// How attn_paged_fwd divides a problem: wavefronts of 32 rows and groups of such wavefronts over the keys (as WaveGroups), workgroups.
+struct PagedShape { int waves, groups, slots; };
+PagedShape paged_shape(int64_t rows, int B, int d);
+size_t paged_part_bytes(const PagedShape& s, int d);
+
+int launch_rotary(const RotaryCall& c, int dtype, hipStream_t s);
+int launch_append(const AppendCall& c, int dtype, hipStream_t s);
+int launch_paged_fwd(const PagedCall& c, const PagedShape& shape, int dtype, hipStream_t s);
+// pairs: host memory, (source, destination) page numbers, checked by the caller; bytes of a row: d * 2.
+struct CopyCall {
+  void* Kc; void* Vc;
+  int layers, Hk, page_size, d;
+  int64_t sl, sp, sh, sn;
+};
+int launch_page_copy(const CopyCall& c, const int* pairs, int64_t n_pairs, hipStream_t s);
+
+}  // namespace attn
