@@ -71,14 +71,21 @@ struct PagedCall {
   float scale_log2;       // tau * log2(e)
 };
 
-// How attn_paged_fwd divides a problem: wavefronts of 32 rows and groups of such wavefronts over the keys (as WaveGroups), workgroups.
-struct PagedShape { int waves, groups, slots; };
-PagedShape paged_shape(int64_t rows, int B, int d);
-size_t paged_part_bytes(const PagedShape& s, int d);
+// How attn_paged_fwd runs: blocks of 32 rows, a wavefront each (attn_paged_one.hip), or of 256 (attn_paged_rows.hip), and the workgroups that share the work.
+struct PagedShape { int rows, slots; };
+int paged_one_slots(int d);
+// Few rows a sequence, on average: single tokens.  (The blocks of 256 rows stream K and V as well for few rows, but in one workgroup per compute unit.)
+inline PagedShape paged_shape(int64_t rows, int B, int d) {
+  if (rows <= (int64_t)32 * B) return {32, paged_one_slots(d)};
+  return {256, kComputeUnits * (d == 128 ? 1 : (d == 64 ? 1 : 2))};
+}
+// Two pieces a slot: 32-bit rows of O and three statistics (Piece in attn_paged_line.h).
+inline size_t paged_part_bytes(const PagedShape& s, int d) { return (size_t)2 * s.slots * s.rows * ((d <= 32 ? 32 : d) + 4) * sizeof(float); }
 
 int launch_rotary(const RotaryCall& c, int dtype, hipStream_t s);
 int launch_append(const AppendCall& c, int dtype, hipStream_t s);
-int launch_paged_fwd(const PagedCall& c, const PagedShape& shape, int dtype, hipStream_t s);
+int launch_paged_one(const PagedCall& c, int dtype, hipStream_t s);
+int launch_paged_rows(const PagedCall& c, int dtype, hipStream_t s);
 // pairs: host memory, (source, destination) page numbers, checked by the caller; bytes of a row: d * 2.
 struct CopyCall {
   void* Kc; void* Vc;

@@ -103,8 +103,8 @@ int check_paged(const attn_paged_params* p, attn::PagedCall* out, attn::PagedSha
   c.scale_log2 = (float)((double)p->softmax_scale * 1.4426950408889634);
   *shape = attn::paged_shape((int64_t)p->T * c.G, p->B, p->d);
   c.slots = shape->slots;
-  // the line that the work is laid out on (attn_paged.hip), at its longest, times the slots, in 62 bits
-  const double rows = (double)p->T * c.G, blocks = rows / (32 * shape->waves) + p->B;
+  // the line that the work is laid out on (attn_paged_line.h), at its longest, times the slots, in 62 bits
+  const double rows = (double)p->T * c.G, blocks = rows / shape->rows + p->B;
   if (p->Hk * (blocks * c.G * ((double)c.b.capacity + 64) + rows * (blocks + 1)) > 0x1p50) return ATTN_ERR_SHAPE;
   return ATTN_OK;
 }
@@ -193,7 +193,8 @@ int attn_paged_fwd(const attn_paged_params* p, const void* Q, const void* k_cach
   if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < attn::paged_part_bytes(shape, p->d)) return ATTN_ERR_WORKSPACE;
   c.Q = Q; c.K = k_cache; c.V = v_cache; c.O = O; c.LSE = LSE;
   c.part = (float*)workspace;
-  return attn::launch_paged_fwd(c, shape, p->dtype, (hipStream_t)p->stream) == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
+  const int e = shape.rows == 32 ? attn::launch_paged_one(c, p->dtype, (hipStream_t)p->stream) : attn::launch_paged_rows(c, p->dtype, (hipStream_t)p->stream);
+  return e == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 
 int attn_paged_copy(const attn_paged_copy_params* p, void* k_cache, void* v_cache, const int32_t* pairs, int64_t n_pairs) {

@@ -1,0 +1,234 @@
+// Attention over a paged cache for many rows a sequence (chunks of a prompt), gfx950.
+//
+// Hundreds of rows use every tile of K and V: the matrix and the vector units bound it.  Arithmetic, register layout and schedule are those of the dense forward with two
+// wavefront groups in ping-pong (attn_fwd_pp.hip): 8 wavefronts of 32 rows, one group a block behind the other, so that one issues MFMA while the other
+// does its softmax; K and V tiles of 64 keys in rings of three, group A copies K and group B V.
+//   Pages: a wavefront copies 16 rows of a tile, which lie in one page.  Its page number is a lane of a register that holds those of sixteen tiles, loaded sixteen tiles
+// ahead: the address of a copy is scalar work alone.  (One load a tile, used in the next, makes the compiler wait for the copies issued since: its count
+// of loads in flight does not know them.)
+//   Blocks of 256 rows; the stretches of the line (attn_paged_line.h) make up for blocks of unequal length, short batches and single tokens in between.
+#include "attn_paged_line.h"
+
+namespace attn {
+namespace {
+
+typedef Division<256, 256, 8> Div;
+constexpr int BR = Div::BR, BC = 64, NT = 512;
+
+template <typename T, int D>
+__global__ __launch_bounds__(NT) void paged_rows_kernel(const PagedCall c) {
+  typedef typename Vec<T>::x8 T8;
+  constexpr int KK = D / 16, DB = D / 32, CPR = D / 8, RPC = 64 / CPR, COPIES = 16 / RPC;
+  __shared__ __attribute__((aligned(16))) T Ks[3][BC * D];
+  __shared__ __attribute__((aligned(16))) T Vs[3][BC * D];
+
+  int slot;
+  Point at;
+  Sequence s;
+  int64_t x_end;
+  if (!stretch<Div>(c, slot, at, s, x_end)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool group_b = wave >= 4;
+  const int part = wave & 3;   // rows 16 part .. + 15 of a tile are this wavefront's to copy
+  const float cs = c.scale_log2;
+  const int page_mask = (1 << c.b.page_log2) - 1;
+
+  while (true) {
+    const int64_t length = s.length(at.t);
+    const int64_t z1 = min(x_end - at.at, length);
+    const bool whole = at.z == 0 && z1 == length;
+    const int tiles = tiles_of<BR>(c, s, at.t, BC);
+    const int j0 = cut_at(at.z, length, tiles), J = cut_at(z1, length, tiles) - j0;   // tiles j0 .. j0 + J - 1
+    const int L = s.L, row0 = at.t * BR + 32 * wave;
+    const bool valid = row0 < s.rows;   // wavefronts past the end only keep the barriers company
+    // (a lane number that the compiler does not derive things from ahead of the loop over items)
+    const int lane = lane_id_here(), r = lane & 31, g = lane >> 5;
+    const Rows w = rows_of(c, s, at.h, row0, r);
+
+    f32x16 o[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+    f32x4 lr_run = {0.f, 0.f, 0.f, 0.f};
+
+    if (J > 0) {
+      const T* const Tg = (const T*)(group_b ? c.V : c.K) + (int64_t)at.h * c.b.sh;   // what this group copies
+      const int* const table = c.b.table + (int64_t)at.b * c.b.table_stride;
+      if (D == 32 && c.d < D) {   // head dimension 16: the copies leave columns >= 16 untouched
+        zero_tiles(&Ks[0][0], 3 * BC * D);
+        zero_tiles(&Vs[0][0], 3 * BC * D);
+        __syncthreads();
+      }
+      uint32_t goff[COPIES];   // byte offset of this lane's chunk of a copy from the first of the 16 rows
+      bool beyond = false;     // D = 32: that chunk lies beyond the tensors' columns
+#pragma unroll
+      for (int p = 0; p < COPIES; ++p) {
+        const int row = p * RPC + lane / CPR, chunk = (lane % CPR) ^ swz_bits<D>(16 * part + row);
+        goff[p] = (uint32_t)(((int64_t)row * c.b.sn + 8 * chunk) * (int64_t)sizeof(T));
+        if (D == 32) beyond = 8 * chunk >= c.d;
+      }
+      // page numbers of the 16-row groups of sixteen tiles from `tile` on (a multiple of sixteen), one a lane
+      auto page_numbers = [&](int tile) { return table[min(tile * BC + 16 * lane, L - 1) >> c.b.page_log2]; };
+      int ids = page_numbers(j0 & ~15), ids_next = ids;
+      int window = j0 & ~15;
+      auto copy_tile = [&](int j, T* lds_tile) {
+        if ((j & ~15) != window) {
+          window = j & ~15;
+          ids = ids_next;
+          ids_next = page_numbers(window + 16);
+        }
+        const int id = __builtin_amdgcn_readlane(ids, 4 * (j & 15) + part);
+        const int row = j * BC + 16 * part;
+        const T* const base = Tg + (int64_t)id * c.b.sp + (int64_t)(row & page_mask) * c.b.sn;
+        const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_addr(lds_tile) + part * COPIES * 1024);
+        if (row + 16 <= L && (uint32_t)id < (uint32_t)c.b.pages) {
+          if (!beyond) {
+#pragma unroll
+            for (int p = 0; p < COPIES; ++p) async_copy_b128(base, goff[p], lds + p * 1024);
+          }
+        } else {
+          const int lane_row = lane_id_here() / CPR;
+          if (!beyond) {
+#pragma unroll
+            for (int p = 0; p < COPIES; ++p) {
+              const bool there = (uint32_t)id < (uint32_t)c.b.pages && row + p * RPC + lane_row < L;
+              async_copy_b128(there ? (const void*)((const char*)base + goff[p]) : (const void*)zero_line, lds + p * 1024);
+            }
+          }
+        }
+      };
+
+      T8 qf[KK];
+      const T* const q_row = (const T*)c.Q + (int64_t)w.token * c.qt + (int64_t)w.head * c.qh;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        if (D == 32 && 16 * kk + 8 * g >= c.d) {   // head dimension 16: the upper columns are zeros
+#pragma unroll
+          for (int e = 0; e < 8; ++e) qf[kk][e] = (T)0.f;
+        } else {
+          qf[kk] = *(const T8*)(q_row + 16 * kk + 8 * g);
+        }
+      }
+      const int pos = w.pos;
+      int calm = kFirstTile;
+      const T8 ones = row_sum_ones<T>();
+      TrOffsets<D> tro;
+      tro.init();
+      f32x16 st[2];
+      T8 pf[4];
+      auto active = [&](int i) { return valid && (j0 + i) * BC <= w.pos_last; };
+
+      constexpr int PF = 4;
+      auto k_frag = [&](const T* kbuf, int f) {  // f = 2 * kk + kb
+        return *(const T8*)(kbuf + lds_off<D>(32 * (f & 1) + r, 2 * (f >> 1) + g));
+      };
+      auto v_frag = [&](const T* vbuf, int f) {  // f = DB * cc + db: consecutive MFMAs hit different accumulators
+        const T* base = vbuf + 16 * (f / DB) * D;
+        return tr_frag<T8>(base + tro.off[f % DB][0], base + tro.off[f % DB][1]);
+      };
+      // M block: O^T += V^T P^T (if do_pv) followed by S^T = K Q^T (if do_s), as one software-pipelined stream
+      auto do_M = [&](bool do_pv, const T* vbuf, bool do_s, const T* kbuf) {
+        constexpr int NV = 4 * DB, NK = 2 * KK;
+        T8 ring[PF];
+        if (do_pv) {
+#pragma unroll
+          for (int f = 0; f < PF; ++f) ring[f] = v_frag(vbuf, f);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int f = 0; f < NV; ++f) {
+            const T8 cur = ring[f % PF];
+            o[f % DB] = mfma32(cur, pf[f / DB], o[f % DB]);
+            if (f + PF < NV) ring[f % PF] = v_frag(vbuf, f + PF);
+            else if (do_s) ring[f % PF] = k_frag(kbuf, f + PF - NV);
+            __builtin_amdgcn_sched_barrier(0);   // keep the prefetch distance the source states
+          }
+        } else if (do_s) {
+#pragma unroll
+          for (int f = 0; f < PF; ++f) ring[f] = k_frag(kbuf, f);
+        }
+        if (do_s) {
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st[kb][i] = 0.f;
+#pragma unroll
+          for (int f = 0; f < NK; ++f) {
+            const int ring_slot = do_pv ? (NV + f) % PF : f % PF;
+            const T8 cur = ring[ring_slot];
+            st[f & 1] = mfma32(cur, qf[f >> 1], st[f & 1]);
+            if (f + PF < NK) ring[ring_slot] = k_frag(kbuf, f + PF);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      };
+      auto ring = [&](int k) -> T* { return group_b ? Vs[k] : Ks[k]; };
+
+      copy_tile(j0, ring(0));
+      wait_async_copies();   // (and Q)
+      ids_next = page_numbers((j0 & ~15) + 16);
+      if (J > 1) copy_tile(j0 + 1, ring(1));
+      __syncthreads();
+      if (group_b) {
+        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();   // B runs one block behind A
+      }
+      int cur = 0;   // ring slot of tile i
+      for (int i = 0; i < J; ++i) {
+        const int nxt = cur == 2 ? 0 : cur + 1, prv = cur == 0 ? 2 : cur - 1;
+        do_M(i > 0 && active(i - 1), Vs[prv], active(i), Ks[cur]);
+        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+        const bool more = i + 2 < J;
+        if (more) copy_tile(j0 + i + 2, ring(prv));
+        if (active(i)) {
+          const KArgs no_dropout = {};
+          softmax_tile_lane_query<T, DB, true, false, false>(no_dropout, st, o, pf, m_run, l_run, lr_run, calm, ones, cs, (j0 + i) * BC, w.pos_first, pos, L, g, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) wait_async_copies_but<COPIES>(); else wait_async_copies();
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+        cur = nxt;
+      }
+      do_M(active(J - 1), Vs[cur == 0 ? 2 : cur - 1], false, Ks[0]);
+      if (!group_b) { __builtin_amdgcn_sched_barrier(0); __syncthreads(); }  // equal barrier counts
+      __builtin_amdgcn_sched_barrier(0);
+      __syncthreads();   // every wavefront is done with the tiles: the buffers become output staging
+    }
+
+    if (valid) {
+      const float l_tot = l_run + xchg32(l_run), lr_sum = lr_run[0];
+      if (whole) {
+        T* const stage = wave < 4 ? &Ks[0][0] + wave * 32 * D : &Vs[0][0] + (wave - 4) * 32 * D;
+        write_rows<T, D>(c, s, at.h, row0, o, m_run, l_tot, lr_sum, stage);
+      } else {
+        write_piece<D, BR>(c, s, at.t, 32 * wave, piece_index(slot, at.z == 0), o, m_run, l_tot, lr_sum);
+      }
+    }
+    const int64_t x = at.at + length;
+    if (x >= x_end || !next_item<BR>(c, x, at, s)) break;
+    __syncthreads();   // the buffers are free again
+  }
+}
+
+template <typename T, int D> int launch(const PagedCall& c, hipStream_t s) {
+  hipLaunchKernelGGL((paged_rows_kernel<T, D>), dim3(c.slots), dim3(NT), 0, s, c);
+  const int e = (int)hipGetLastError();
+  if (e != 0) return e;
+  hipLaunchKernelGGL((paged_join_kernel<T, D, Div>), dim3(c.slots - 1), dim3(512), 0, s, c);
+  return (int)hipGetLastError();
+}
+template <typename T> int launch_t(const PagedCall& c, hipStream_t s) {
+  if (c.d <= 32) return launch<T, 32>(c, s);
+  if (c.d == 64) return launch<T, 64>(c, s);
+  return launch<T, 128>(c, s);
+}
+
+}  // namespace
+
+int launch_paged_rows(const PagedCall& c, int dtype, hipStream_t s) { return dtype == ATTN_FP16 ? launch_t<_Float16>(c, s) : launch_t<__bf16>(c, s); }
+
+}  // namespace attn
