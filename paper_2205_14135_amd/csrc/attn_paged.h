@@ -79,8 +79,11 @@ inline PagedShape paged_shape(int64_t rows, int B, int d) {
   if (rows <= (int64_t)32 * B) return {32, paged_one_slots(d)};
   return {256, kComputeUnits * (d == 128 ? 1 : (d == 64 ? 1 : 2))};
 }
-// Two pieces a slot: 32-bit rows of O and three statistics (Piece in attn_paged_line.h).
-inline size_t paged_part_bytes(const PagedShape& s, int d) { return (size_t)2 * s.slots * s.rows * ((d <= 32 ? 32 : d) + 4) * sizeof(float); }
+// The number of slots and what to join at each of them (Join in attn_paged_line.h), then two pieces a slot: 32-bit rows of O and three statistics (Piece).
+constexpr int kJoinBytes = 32;
+inline size_t paged_part_bytes(const PagedShape& s, int d) {
+  return (size_t)(s.slots + 1) * kJoinBytes + (size_t)2 * s.slots * s.rows * ((d <= 32 ? 32 : d) + 4) * sizeof(float);
+}
 
 int launch_rotary(const RotaryCall& c, int dtype, hipStream_t s);
 int launch_append(const AppendCall& c, int dtype, hipStream_t s);

@@ -24,28 +24,35 @@ struct Sequence {
   __device__ __forceinline__ int64_t length(int t) const { return a + (int64_t)step * (t + 1); }
   __device__ __forceinline__ int64_t upto(int64_t t) const { return t * a + step * (t * (t + 1) / 2); }
 };
-// UNIFORM: b is the same in all lanes, and so is what comes back, in scalar registers.
-template <int BR, bool UNIFORM = true> __device__ __forceinline__ Sequence sequence(const PagedCall& c, int b) {
+template <int BR> __device__ __forceinline__ Sequence sequence_of(const PagedCall& c, int first, int m, int L) {
   Sequence s;
-  const PagedBatch& p = c.b;
-  auto number = [](int v) { return UNIFORM ? __builtin_amdgcn_readfirstlane(v) : v; };
-  s.L = min(max(number(p.lengths[b]), 0), p.capacity);
-  int end;
-  if (p.starts) {
-    const int first = number(p.starts[b]);
-    end = number(p.starts[b + 1]);
-    s.first = min(max(first, 0), p.T);
-    end = min(max(end, s.first), p.T);
-  } else {
-    s.first = b;
-    end = b + 1;   // (the host checks T >= B)
-  }
-  s.m = end - s.first;
-  s.rows = s.m * c.G;
+  s.first = first;
+  s.m = m;
+  s.L = L;
+  s.rows = m * c.G;
   s.blocks = (s.rows + BR - 1) / BR;
-  s.a = (int64_t)c.G * ((c.causal ? max(s.L - s.m, 0) : s.L) + kItemKeys);
+  s.a = (int64_t)c.G * ((c.causal ? max(L - m, 0) : L) + kItemKeys);
   s.step = c.causal ? BR : 0;
   return s;
+}
+// Sequence b (one a lane)
+template <int BR> __device__ __forceinline__ Sequence load_sequence(const PagedCall& c, int b) {
+  const PagedBatch& p = c.b;
+  const int L = min(max(p.lengths[b], 0), p.capacity);
+  int first = b, end = b + 1;   // (the host checks T >= B)
+  if (p.starts) {
+    first = min(max(p.starts[b], 0), p.T);
+    end = min(max(p.starts[b + 1], first), p.T);
+  }
+  return sequence_of<BR>(c, first, end - first, L);
+}
+// the same for one that all lanes share, in scalar registers
+template <int BR> __device__ __forceinline__ Sequence load_sequence_uniform(const PagedCall& c, int b) {
+  const Sequence s = load_sequence<BR>(c, b);
+  return sequence_of<BR>(c, __builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.m), __builtin_amdgcn_readfirstlane(s.L));
+}
+template <int BR> __device__ __forceinline__ Sequence lane_sequence(const PagedCall& c, const Sequence& s, int lane) {
+  return sequence_of<BR>(c, __builtin_amdgcn_readlane(s.first, lane), __builtin_amdgcn_readlane(s.m, lane), __builtin_amdgcn_readlane(s.L, lane));
 }
 
 __device__ __forceinline__ int64_t lane64(int64_t v, int lane) {
@@ -65,36 +72,39 @@ struct Point {
   int64_t at, z;
 };
 
-// The line, seen by one wavefront: lane i of a round over 64 sequences has the length of sequence (round + i), summed up to it.
+// 64 sequences of the line, one a lane: its stretch, and the sum up to its end.
+struct Round {
+  Sequence s;
+  int64_t cost, incl;
+  template <int BR> __device__ __forceinline__ void load(const PagedCall& c, int b0) {
+    const int lane = threadIdx.x & 63, n = c.b.B - b0;
+    s = load_sequence<BR>(c, b0 + min(lane, n - 1));
+    cost = lane < n ? s.upto(s.blocks) * c.b.Hk : 0;
+    incl = cost;
+    for (int d = 1; d < min(n, 64); d <<= 1) {
+      const int64_t other = __shfl_up(incl, d, 64);
+      if (lane >= d) incl += other;
+    }
+  }
+};
+
+// The line, seen by one wavefront.
 template <int BR> struct Line {
   int64_t total;
-  int64_t incl0, cost0;   // of the first round, which is all there is for up to 64 sequences
+  Round first;            // all there is for up to 64 sequences
   int n;                  // slots that get a stretch
   int64_t each;           // stretches are `each` long, the first `longer` one more
   int longer;
   int64_t slack;          // a cut nearer than this to an item's end is made there
 
-  __device__ __forceinline__ void round(const PagedCall& c, int b0, int64_t& cost, int64_t& incl) const {
-    const int lane = threadIdx.x & 63;
-    cost = 0;
-    if (b0 + lane < c.b.B) {
-      const Sequence s = sequence<BR, false>(c, b0 + lane);
-      cost = s.upto(s.blocks) * c.b.Hk;
-    }
-    incl = cost;
-    for (int d = 1; d < min(c.b.B - b0, 64); d <<= 1) {
-      const int64_t other = __shfl_up(incl, d, 64);
-      if (lane >= d) incl += other;
-    }
-  }
   // least: keys that a stretch has at least, with what an item costs
   __device__ __forceinline__ void init(const PagedCall& c, int least, int slack_share) {
-    round(c, 0, cost0, incl0);
-    total = lane64(incl0, min(c.b.B, 64) - 1);
+    first.load<BR>(c, 0);
+    total = lane64(first.incl, min(c.b.B, 64) - 1);
     for (int b0 = 64; b0 < c.b.B; b0 += 64) {
-      int64_t cost, incl;
-      round(c, b0, cost, incl);
-      total += lane64(incl, min(c.b.B - b0, 64) - 1);
+      Round r;
+      r.load<BR>(c, b0);
+      total += lane64(r.incl, min(c.b.B - b0, 64) - 1);
     }
     const int64_t worth = divided(total, (int64_t)(least + kItemKeys) * c.G);
     n = (int)(worth < 1 ? 1 : (worth > c.slots ? c.slots : worth));
@@ -103,28 +113,33 @@ template <int BR> struct Line {
     slack = slack_share > 0 ? each / slack_share : 0;
   }
   __device__ __forceinline__ int64_t start(int slot) const { return each * slot + min(slot, longer); }
-  __device__ __forceinline__ Point locate(const PagedCall& c, int64_t x) const {   // 0 <= x < total
+  // The item at 0 <= x < total, and its sequence.
+  __device__ __forceinline__ Point locate(const PagedCall& c, int64_t x, Sequence& s) const {
     Point p;
-    int64_t before = 0, cost = cost0, incl = incl0;
+    int64_t before = 0;
+    Round r = first;
     for (int b0 = 0;; b0 += 64) {
-      if (b0 > 0) round(c, b0, cost, incl);
+      if (b0 > 0) r.load<BR>(c, b0);
       const int in_round = min(c.b.B - b0, 64);
-      const uint64_t beyond = __ballot((int)(threadIdx.x & 63) < in_round && before + incl > x);
+      const uint64_t beyond = __ballot((int)(threadIdx.x & 63) < in_round && before + r.incl > x);
       if (beyond != 0 || b0 + 64 >= c.b.B) {
         const int i = beyond != 0 ? __builtin_ctzll(beyond) : in_round - 1;
         p.b = b0 + i;
-        p.at = before + lane64(incl, i) - lane64(cost, i);
+        p.at = before + lane64(r.incl, i) - lane64(r.cost, i);
+        s = lane_sequence<BR>(c, r.s, i);
         break;
       }
-      before += lane64(incl, 63);
+      before += lane64(r.incl, 63);
     }
-    const Sequence s = sequence<BR>(c, p.b);
-    const int64_t head = s.upto(s.blocks), in = x - p.at;
-    int h = (int)divided(in, head);
-    const int64_t y = in - h * head;
-    // t with S(t) <= y < S(t + 1)
-    int t = 0;
-    if (s.blocks > 1) {
+    const int64_t in = x - p.at;
+    int64_t head = s.a + s.step;
+    int h, t = 0;
+    if (s.blocks == 1) {
+      h = (int)divided(in, head);
+    } else {
+      head = s.upto(s.blocks);
+      h = (int)divided(in, head);
+      const int64_t y = in - h * head;   // t with S(t) <= y < S(t + 1)
       if (s.step == 0) {
         t = (int)divided(y, s.a);
       } else {
@@ -137,12 +152,18 @@ template <int BR> struct Line {
     }
     p.t = __builtin_amdgcn_readfirstlane(t);
     p.h = __builtin_amdgcn_readfirstlane(h);
-    p.b = __builtin_amdgcn_readfirstlane(p.b);
-    p.at = lane64(p.at + p.h * head + s.upto(p.t), 0);
+    p.at += p.h * head + s.upto(p.t);
     p.z = x - p.at;
     return p;
   }
 };
+
+// What the second kernel joins at a slot: pieces (0: nothing) of the slots from the one before on, rows `row0` to row0 + rows - 1 of K head h of the sequence
+// whose first token is `first`.
+struct Join { int pieces, row0, rows, first, h, unused[3]; };
+static_assert(sizeof(Join) == kJoinBytes, "the workspace counts them");
+__device__ __forceinline__ int* join_slots(const PagedCall& c) { return (int*)c.part; }
+__device__ __forceinline__ Join* join_list(const PagedCall& c) { return (Join*)((char*)c.part + kJoinBytes); }
 
 // How a kernel divides its line: rows of a block, keys of a stretch at least, and the share of a stretch (0: none) that a cut is moved by to an item's end.
 template <int BR_, int LEAST, int SLACK> struct Division {
@@ -159,25 +180,42 @@ template <int BR> __device__ __forceinline__ bool next_item(const PagedCall& c, 
   at.h = 0;
   do {
     if (++at.b >= c.b.B) return false;
-    s = sequence<BR>(c, at.b);
+    s = load_sequence_uniform<BR>(c, at.b);
   } while (s.rows == 0);
   return true;
 }
 
-// The stretch of a slot: from `at` (s: its sequence) to x_end.  False: there is none.
+// The stretch of a slot: from `at` (s: its sequence) to x_end.  False: there is none.  Leaves in the workspace how many slots there are, and for the first
+// cut of an item what is to be joined there.
 template <class DIV> __device__ __forceinline__ bool stretch(const PagedCall& c, int& slot, Point& at, Sequence& s, int64_t& x_end) {
   constexpr int BR = DIV::BR;
   Line<BR> line;
   DIV::init(line, c);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *join_slots(c) = line.total == 0 ? 0 : line.n;
   slot = xcd_item(line.n, (line.n + kXcds - 1) / kXcds);   // neighbours on the line share an XCD's L2
   if (slot < 0 || line.total == 0) return false;
-  at = line.locate(c, line.start(slot));
-  s = sequence<BR>(c, at.b);
+  at = line.locate(c, line.start(slot), s);
+  if (slot > 0) {
+    const int64_t near_end = at.at + s.length(at.t) - line.slack;
+    int pieces = 0;
+    if (at.z > line.slack && line.start(slot) < near_end && line.start(slot - 1) - at.at <= line.slack) {
+      // slots slot - 1 to the last that starts in the item: the smallest k with start(k) >= near_end
+      int k = (int)min((int64_t)line.n, divided(max(near_end - line.longer, (int64_t)0), line.each));
+      while (k < line.n && line.start(k) < near_end) ++k;
+      while (line.start(k - 1) >= near_end) --k;
+      pieces = k - (slot - 1);
+    }
+    if (threadIdx.x == 0) {
+      const Join j = {pieces, at.t * BR, min(BR, s.rows - at.t * BR), s.first, at.h, {0, 0, 0}};
+      join_list(c)[slot] = j;
+    }
+  }
   x_end = line.start(slot + 1);
   if (line.slack > 0) {
     if (slot + 1 < line.n) {
-      const Point e = line.locate(c, x_end);
-      const int64_t v = sequence<BR>(c, e.b).length(e.t);
+      Sequence last;
+      const Point e = line.locate(c, x_end, last);
+      const int64_t v = last.length(e.t);
       if (e.z <= line.slack) x_end = e.at;
       else if (v - e.z <= line.slack) x_end = e.at + v;
     }
@@ -260,117 +298,11 @@ __device__ __forceinline__ void write_rows(const PagedCall& c, const Sequence& s
   __builtin_amdgcn_wave_barrier();
 }
 
-// A cut item's piece in the workspace: rows of O, not yet divided by the sum, and (m, l, sum of the rounded probabilities) of every row.
-template <int D, int BR> struct Piece {
-  static constexpr int kFloats = BR * (D + 4);
-  float* o;
-  float* s;
-  __device__ __forceinline__ Piece(const PagedCall& c, int index) {
-    o = c.part + (int64_t)index * kFloats;
-    s = o + BR * D;
-  }
-};
+// A cut item's pieces in the workspace: O, not yet divided by the sum, and (m, l, sum of the rounded probabilities) of its rows, kFloats = BR (D + 4) floats.
+template <int D, int BR> __device__ __forceinline__ float* piece_of(const PagedCall& c, int index) {
+  return (float*)((char*)c.part + (int64_t)(c.slots + 1) * kJoinBytes) + (int64_t)index * (BR * (D + 4));
+}
 // Its index: a slot has at most one piece that starts inside an item and one that does not.
 __device__ __forceinline__ int piece_index(int slot, bool from_start) { return 2 * slot + (from_start ? 1 : 0); }
-
-// 32 rows of a piece, from row0 of the block on (row0 + 32 t of the item's rows exist up to s.rows).
-template <int D, int BR>
-__device__ __forceinline__ void write_piece(const PagedCall& c, const Sequence& s, int t, int row0, int index, const f32x16 (&o)[D / 32], float m_run, float l_tot,
-                                            float lr_sum) {
-  const int lane = lane_id_here(), r = lane & 31, g = lane >> 5;
-  if (t * BR + row0 + r >= s.rows) return;
-  const Piece<D, BR> piece(c, index);
-  float* const row = piece.o + (row0 + r) * D;
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int i4 = 0; i4 < 4; ++i4) {
-      const f32x4 v = {o[db][4 * i4], o[db][4 * i4 + 1], o[db][4 * i4 + 2], o[db][4 * i4 + 3]};
-      *(f32x4*)(row + 32 * db + 8 * i4 + 4 * g) = v;
-    }
-  if (g == 0) {
-    const f32x4 v = {m_run, l_tot, lr_sum, 0.f};
-    *(f32x4*)(piece.s + 4 * (row0 + r)) = v;
-  }
-}
-
-// Joins the pieces of the items that were cut.  The workgroup of slot i (from 1 on) looks at the cut at the start of that slot's stretch, and does the item if the
-// cut is its first one.  A wavefront does a row: lane k weighs piece k, then the lanes are columns.  One piece after the other, rows in the accumulators' layout, took
-// 98.6 us for the 16 items of two contexts of 10^5 tokens (16 pieces each), mostly waiting.
-template <typename T, int D, class DIV>
-__global__ __launch_bounds__(512) void paged_join_kernel(const PagedCall c) {
-  constexpr int BR = DIV::BR;
-  Line<BR> line;
-  DIV::init(line, c);
-  const int slot = (int)blockIdx.x + 1;
-  if (slot >= line.n) return;
-  const Point at = line.locate(c, line.start(slot));
-  const Sequence s = sequence<BR>(c, at.b);
-  const int64_t length = s.length(at.t), near_end = at.at + length - line.slack;   // (stretch() above makes the same cuts)
-  if (at.z <= line.slack || line.start(slot) >= near_end || line.start(slot - 1) - at.at > line.slack) return;   // no cut, or not the first one
-  int pieces = 2;   // of the slots from slot - 1 on
-  while (slot - 1 + pieces < line.n && line.start(slot - 1 + pieces) < near_end) ++pieces;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rows = min(BR, s.rows - at.t * BR);
-  constexpr int C = D / 64 > 0 ? D / 64 : 1;   // columns of a lane
-  const int col = C * lane;
-  for (int row = wave; row < rows; row += 8) {
-    // the item's statistic: rounds of 64 pieces
-    float m = -INFINITY;
-    for (int k0 = 0; k0 < pieces; k0 += 64) {
-      const int k = k0 + lane;
-      float mk = -INFINITY;
-      if (k < pieces) mk = Piece<D, BR>(c, piece_index(slot - 1 + k, k == 0)).s[4 * row];
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) mk = fmaxf(mk, __shfl_xor(mk, d, 64));
-      m = fmaxf(m, mk);
-    }
-    const float ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f, lr = 0.f, acc[C];
-#pragma unroll
-    for (int e = 0; e < C; ++e) acc[e] = 0.f;
-    for (int k0 = 0; k0 < pieces; k0 += 64) {
-      const int k = k0 + lane, n = min(64, pieces - k0);
-      float wk = 0.f, lk = 0.f, rk = 0.f;
-      if (k < pieces) {
-        const f32x4 st = *(const f32x4*)(Piece<D, BR>(c, piece_index(slot - 1 + k, k == 0)).s + 4 * row);
-        wk = __builtin_amdgcn_exp2f(st[0] - ref);
-        lk = st[1] * wk;
-        rk = st[2] * wk;
-      }
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        lk += __shfl_xor(lk, d, 64);
-        rk += __shfl_xor(rk, d, 64);
-      }
-      l += lk;
-      lr += rk;
-      for (int i0 = 0; i0 < n; i0 += 8) {   // eight loads in flight
-        float v[8][C];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int piece = min(k0 + i0 + i, pieces - 1);
-          const float* const o = Piece<D, BR>(c, piece_index(slot - 1 + piece, piece == 0)).o + row * D + min(col, D - C);
-#pragma unroll
-          for (int e = 0; e < C; ++e) v[i][e] = o[e];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float w = i0 + i < n ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wk), (i0 + i) & 63)) : 0.f;
-#pragma unroll
-          for (int e = 0; e < C; ++e) acc[e] += i0 + i < n ? v[i][e] * w : 0.f;
-        }
-      }
-    }
-    const float inv = (l > 0.f && lr > 0.f) ? 1.f / lr : (l == l ? 0.f : l);   // (a row of NaN stays one)
-    const int i = (at.t * BR + row) / c.G, head = at.h * c.G + (at.t * BR + row) % c.G, token = s.first + i;
-    if (lane == 0) c.LSE[(int64_t)head * c.b.T + token] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : (l == l ? -INFINITY : l);
-    if (col < c.d) {
-      T* const dst = (T*)c.O + (int64_t)token * c.ot + (int64_t)head * c.oh + col;
-#pragma unroll
-      for (int e = 0; e < C; ++e) dst[e] = (T)(acc[e] * inv);
-    }
-  }
-}
 
 }  // namespace attn

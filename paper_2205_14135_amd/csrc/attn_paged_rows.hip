@@ -15,6 +15,66 @@ namespace {
 typedef Division<256, 256, 8> Div;
 constexpr int BR = Div::BR, BC = 64, NT = 512;
 
+// A piece in the layout of the accumulators: 16 bytes a lane at a time, whole lines; then the statistics of every wavefront's 32 rows.
+template <int D> __device__ __forceinline__ f32x4* piece_o(float* piece, int wave, int lane) { return (f32x4*)piece + wave * (8 * D) + lane; }
+template <int D> __device__ __forceinline__ f32x4* piece_s(float* piece, int wave, int lane) { return (f32x4*)(piece + BR * D) + 32 * wave + (lane & 31); }
+template <int D> __device__ __forceinline__ void write_piece(const PagedCall& c, int wave, int index, const f32x16 (&o)[D / 32], float m_run, float l_tot, float lr_sum) {
+  const int lane = lane_id_here();
+  float* const piece = piece_of<D, BR>(c, index);
+  f32x4* const po = piece_o<D>(piece, wave, lane);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      const f32x4 v = {o[db][4 * i4], o[db][4 * i4 + 1], o[db][4 * i4 + 2], o[db][4 * i4 + 3]};
+      po[64 * (4 * db + i4)] = v;
+    }
+  if (lane < 32) {
+    const f32x4 v = {m_run, l_tot, lr_sum, 0.f};
+    *piece_s<D>(piece, wave, lane) = v;
+  }
+}
+
+// Joins the pieces of the items that were cut: blockIdx.x + 1 is the slot of an item's first cut; a wavefront does 32 rows.  (Rows one after the other, and lanes as
+// columns, as for single tokens: chunk of 2048 tokens on 14336, two or three pieces of most of 256 items, 32 us.)
+template <typename T, int D>
+__global__ __launch_bounds__(NT) void paged_rows_join_kernel(const PagedCall c) {
+  constexpr int DB = D / 32;
+  __shared__ __attribute__((aligned(16))) T stage[NT / 64][32 * D];
+  const int slot = (int)blockIdx.x + 1;
+  const Join j = join_list(c)[slot];
+  if (slot >= *join_slots(c) || j.pieces == 0) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (32 * wave >= j.rows) return;
+  f32x16 o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  float m = -INFINITY, l = 0.f, lr = 0.f;
+  for (int k = 0; k < j.pieces; ++k) {
+    float* const piece = piece_of<D, BR>(c, piece_index(slot - 1 + k, k == 0));
+    const f32x4* const po = piece_o<D>(piece, wave, lane);
+    const f32x4 st = *piece_s<D>(piece, wave, lane);
+    f32x4 v[4 * DB];
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i) v[i] = po[64 * i];
+    const float top = fmaxf(m, st[0]), ref = top == -INFINITY ? 0.f : top;
+    const float w0 = __builtin_amdgcn_exp2f(m - ref), w1 = __builtin_amdgcn_exp2f(st[0] - ref);
+    m = top;
+    l = l * w0 + st[1] * w1;
+    lr = lr * w0 + st[2] * w1;
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i / 4][4 * (i % 4) + e] = o[i / 4][4 * (i % 4) + e] * w0 + v[i][e] * w1;
+  }
+  Sequence s = {};
+  s.first = j.first;
+  s.rows = j.row0 + j.rows;   // (of the item's sequence, as far as this block goes)
+  write_rows<T, D>(c, s, j.h, j.row0 + 32 * wave, o, m, l, lr, stage[wave]);
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(NT) void paged_rows_kernel(const PagedCall c) {
   typedef typename Vec<T>::x8 T8;
@@ -205,7 +265,7 @@ __global__ __launch_bounds__(NT) void paged_rows_kernel(const PagedCall c) {
         T* const stage = wave < 4 ? &Ks[0][0] + wave * 32 * D : &Vs[0][0] + (wave - 4) * 32 * D;
         write_rows<T, D>(c, s, at.h, row0, o, m_run, l_tot, lr_sum, stage);
       } else {
-        write_piece<D, BR>(c, s, at.t, 32 * wave, piece_index(slot, at.z == 0), o, m_run, l_tot, lr_sum);
+        write_piece<D>(c, wave, piece_index(slot, at.z == 0), o, m_run, l_tot, lr_sum);
       }
     }
     const int64_t x = at.at + length;
@@ -218,7 +278,7 @@ template <typename T, int D> int launch(const PagedCall& c, hipStream_t s) {
   hipLaunchKernelGGL((paged_rows_kernel<T, D>), dim3(c.slots), dim3(NT), 0, s, c);
   const int e = (int)hipGetLastError();
   if (e != 0) return e;
-  hipLaunchKernelGGL((paged_join_kernel<T, D, Div>), dim3(c.slots - 1), dim3(512), 0, s, c);
+  hipLaunchKernelGGL((paged_rows_join_kernel<T, D>), dim3(c.slots - 1), dim3(NT), 0, s, c);
   return (int)hipGetLastError();
 }
 template <typename T> int launch_t(const PagedCall& c, hipStream_t s) {
