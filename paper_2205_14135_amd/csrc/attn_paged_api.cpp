@@ -98,10 +98,12 @@ int check_paged(const attn_paged_params* p, attn::PagedCall* out, attn::PagedSha
   if (!rows_ok({qt, qh, ot, oh}) || !rows_apart(p->d, ot, oh)) return ATTN_ERR_SHAPE;
   c.qt = qt.stride; c.qh = qh.stride; c.ot = ot.stride; c.oh = oh.stride;
   c.G = p->Hq / p->Hk;
+  c.g_shift = 31 + (c.G > 1 ? log2_of(c.G - 1) + 1 : 0);
+  c.g_factor = (uint32_t)((((uint64_t)1 << c.g_shift) + c.G - 1) / c.G);
   c.d = p->d;
   c.causal = p->causal != 0;
   c.scale_log2 = (float)((double)p->softmax_scale * 1.4426950408889634);
-  *shape = attn::paged_shape((int64_t)p->T * c.G, p->B, p->d);
+  *shape = attn::paged_shape((int64_t)p->T * c.G, p->B, p->Hk, p->d);
   c.slots = shape->slots;
   // the line that the work is laid out on (attn_paged_line.h), at its longest, times the slots, in 62 bits
   const double rows = (double)p->T * c.G, blocks = rows / shape->rows + p->B;

@@ -1,28 +1,26 @@
 // Attention over a paged cache for few rows a sequence (single tokens), gfx950.
 //
 // A token of G heads a group reads 4 d bytes of cache for 4 d G operations: the memory bounds it, and what counts is how much of K and V is on its way at any time.
-// A workgroup is one wavefront with tiles of its own, 32 KB of LDS: five to a compute unit, no barriers, 80 KB in flight, and while one of them
-// ends an item and waits for the lengths, page numbers and first tile of the next, the others stream on.
-//   A tile is kKeys keys of K and V.  S^T = K Q^T with 32x32x16 MFMA: a lane holds the logits of one row (G of the 32 are real), online softmax,
+// A workgroup is one wavefront with tiles of its own (d = 128: 48 KB of LDS, three to a compute unit, 96 KB in flight): no barriers, and while one of them
+// ends an item and waits for the page numbers and the first tile of the next, the others stream on.
+//   A tile is 32 keys of K and V.  S^T = K Q^T with 32x32x16 MFMA: a lane holds the logits of one row (G of the 32 are real), online softmax,
 // O^T += V^T P^T; the matrix and vector work is a fifth of what the memory takes.
-//   A page holds 16 rows or more, so a tile is kKeys / 16 page numbers at most, which scalar loads bring two tiles ahead.
+//   A page holds 16 rows or more, so a tile has two page numbers at most, which scalar loads bring a tile ahead.
 #include "attn_paged_line.h"
 
 namespace attn {
 namespace {
 
-typedef Division<32, 64, 0> Div;
+typedef Division<32, 64, 64, 0> Div;
 constexpr int BR = Div::BR;
 
+// (us, the main kernel.  d = 64, tiles of 64 keys | 32: one token over 777 keys 9.5 | 7.6, 32 sequences of up to 2000 35.9 | 35.1 with the join.  d = 128, 64 sequences and two contexts of
+// 10^5 tokens: two tiles of 32 keys and five wavefronts to a compute unit 108, 163; three and three 97, 143; four and two 103, 151; two tiles of 64 and two wavefronts 110, 148.)
 template <int D> struct OneShape {
-  static constexpr int kKeys = D == 128 ? 32 : 64;
-#ifdef V_STAGES
-  static constexpr int kStages = V_STAGES;
-#else
-  static constexpr int kStages = 3;
-#endif
+  static constexpr int kKeys = 32;     // of a tile
+  static constexpr int kStages = 3;    // tiles: one in use, two on their way
   static constexpr int kLds = kStages * 2 * kKeys * D * 2;
-  static constexpr int kPerUnit = 160 * 1024 / kLds;   // wavefronts that a compute unit holds
+  static constexpr int kPerUnit = 160 * 1024 / kLds < 8 ? 160 * 1024 / kLds : 8;   // wavefronts that a compute unit holds
 };
 
 // Online softmax of a tile of 32 NB keys, lane = row (two lanes a row): as softmax_tile_lane_query in attn_common.h, but the reference follows the maximum of every tile,
@@ -87,87 +85,93 @@ __device__ __forceinline__ void write_piece(const PagedCall& c, const Sequence& 
   }
 }
 
-// Joins the pieces of the items that were cut: blockIdx.x + 1 is the slot of an item's first cut.  16 wavefronts; with few rows several of them share a row and take
-// its pieces by eights in turn.  A lane is C columns.
-// (One piece after the other, in the layout of the accumulators: 98.6 us for the 16 items of two contexts of 10^5 tokens, 16 pieces each.)
+// Joins the pieces of the items that were cut: blockIdx.x + 1 is the slot of an item's first cut, blockIdx.y eight of its rows.  The four wavefronts take pieces by
+// fours in turn, 16 bytes of a row a lane, sixteen loads in flight, and meet in LDS.
+// us, the join alone: one piece after the other, rows in the accumulators' layout, 16 items of 16 pieces and 4 rows 98.6; 16 wavefronts an item, a row or a share of
+// one's pieces each, 48 pieces of 4 rows 13.8, but 8 items of 96 pieces and 16 rows about 50.
 template <typename T, int D>
-__global__ __launch_bounds__(1024) void paged_one_join_kernel(const PagedCall c) {
-  constexpr int WAVES = 16, C = D / 64 > 0 ? D / 64 : 1;
-  __shared__ float sums[WAVES][64 * C + 4];
-  const int slot = (int)blockIdx.x + 1;
+__global__ __launch_bounds__(256) void paged_one_join_kernel(const PagedCall c) {
+  constexpr int WAVES = 4, LPR = D / 4, RPI = 64 / LPR, NR = 8 / RPI, NP = 4;   // lanes of a row, rows of a load, loads of a piece, pieces at a time
+  __shared__ f32x4 part_o[WAVES][NR][64];
+  __shared__ f32x4 part_s[WAVES][NR][RPI];
+  const int slot = (int)blockIdx.x + 1, row0 = 8 * (int)blockIdx.y;
   const Join j = join_list(c)[slot];
-  if (slot >= *join_slots(c) || j.pieces == 0) return;
+  if (slot >= *join_slots(c) || j.pieces == 0 || row0 >= j.rows) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rows = j.rows;
-  int share = 1;   // wavefronts of a row
-  while (2 * share * rows <= WAVES && 8 * share < j.pieces) share *= 2;
-  const int col = min(C * lane, D - C), turn = wave % share;
-  for (int r0 = 0; r0 < rows; r0 += WAVES / share) {
-    const bool active = r0 + wave / share < rows;
-    const int row = min(r0 + wave / share, rows - 1);
-    float m = -INFINITY, l = 0.f, lr = 0.f, acc[C];
+  const int sub = lane / LPR, col = 4 * (lane % LPR);
+  f32x4 acc[NR], st[NR];   // st: m, l, sum of the rounded ones
 #pragma unroll
-    for (int e = 0; e < C; ++e) acc[e] = 0.f;
-    for (int k0 = 8 * turn; k0 < j.pieces; k0 += 8 * share) {
-      f32x4 st[8];
-      float v[8][C];
+  for (int n = 0; n < NR; ++n) {
+    acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    st[n] = f32x4{-INFINITY, 0.f, 0.f, 0.f};
+  }
+  for (int k0 = NP * wave; k0 < j.pieces; k0 += NP * WAVES) {
+    f32x4 v[NP][NR], t[NP][NR];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {   // sixteen loads in flight
-        const int k = min(k0 + i, j.pieces - 1);
-        const float* const piece = piece_of<D, BR>(c, piece_index(slot - 1 + k, k == 0));
-        st[i] = *(const f32x4*)(piece + BR * D + 4 * row);
+    for (int i = 0; i < NP; ++i) {
+      const int k = min(k0 + i, j.pieces - 1);
+      const float* const piece = piece_of<D, BR>(c, piece_index(slot - 1 + k, k == 0));
 #pragma unroll
-        for (int e = 0; e < C; ++e) v[i][e] = piece[row * D + col + e];
-      }
-      float top = m;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, st[i][0]);   // (a piece twice: no harm)
-      const float ref = top == -INFINITY ? 0.f : top, w0 = __builtin_amdgcn_exp2f(m - ref);
-      m = top;
-      l *= w0;
-      lr *= w0;
-#pragma unroll
-      for (int e = 0; e < C; ++e) acc[e] *= w0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (k0 + i >= j.pieces) break;
-        const float w = __builtin_amdgcn_exp2f(st[i][0] - ref);
-        l += st[i][1] * w;
-        lr += st[i][2] * w;
-#pragma unroll
-        for (int e = 0; e < C; ++e) acc[e] += v[i][e] * w;
+      for (int n = 0; n < NR; ++n) {
+        const int row = min(row0 + n * RPI + sub, j.rows - 1);
+        t[i][n] = *(const f32x4*)(piece + BR * D + 4 * row);
+        v[i][n] = *(const f32x4*)(piece + row * D + col);
       }
     }
-    if (share > 1) {   // (the same for the whole workgroup)
-      if (r0 > 0) __syncthreads();
 #pragma unroll
-      for (int e = 0; e < C; ++e) sums[wave][C * lane + e] = acc[e];
-      if (lane == 0) {
-        sums[wave][64 * C] = m;
-        sums[wave][64 * C + 1] = l;
-        sums[wave][64 * C + 2] = lr;
-      }
-      __syncthreads();
-      if (turn == 0)
-        for (int k = 1; k < share; ++k) {
-          const float* const other = sums[wave + k];
-          const float mk = other[64 * C], top = fmaxf(m, mk), ref = top == -INFINITY ? 0.f : top;
-          const float w0 = __builtin_amdgcn_exp2f(m - ref), w1 = __builtin_amdgcn_exp2f(mk - ref);
-          m = top;
-          l = l * w0 + other[64 * C + 1] * w1;
-          lr = lr * w0 + other[64 * C + 2] * w1;
+    for (int n = 0; n < NR; ++n) {
+      float top = st[n][0];
 #pragma unroll
-          for (int e = 0; e < C; ++e) acc[e] = acc[e] * w0 + other[C * lane + e] * w1;
+      for (int i = 0; i < NP; ++i) top = fmaxf(top, t[i][n][0]);   // (the last piece more than once: no harm)
+      const float ref = top == -INFINITY ? 0.f : top, w0 = __builtin_amdgcn_exp2f(st[n][0] - ref);
+      st[n][0] = top;
+      st[n][1] *= w0;
+      st[n][2] *= w0;
+      acc[n] *= w0;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const bool there = k0 + i < j.pieces;
+        const float w = __builtin_amdgcn_exp2f(t[i][n][0] - ref);
+        if (there) {
+          st[n][1] += t[i][n][1] * w;
+          st[n][2] += t[i][n][2] * w;
+          acc[n] += v[i][n] * w;
         }
+      }
     }
-    if (turn != 0 || !active) continue;
-    const float inv = (l > 0.f && lr > 0.f) ? 1.f / lr : (l == l ? 0.f : l);   // (a row of NaN stays one)
-    const int i = (j.row0 + row) / c.G, head = j.h * c.G + (j.row0 + row) - i * c.G, token = j.first + i;
-    if (lane == 0) c.LSE[(int64_t)head * c.b.T + token] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : (l == l ? -INFINITY : l);
-    if (C * lane < c.d) {
-      T* const dst = (T*)c.O + (int64_t)token * c.ot + (int64_t)head * c.oh + C * lane;
+  }
 #pragma unroll
-      for (int e = 0; e < C; ++e) dst[e] = (T)(acc[e] * inv);
+  for (int n = 0; n < NR; ++n) {
+    part_o[wave][n][lane] = acc[n];
+    if (col == 0) part_s[wave][n][sub] = st[n];
+  }
+  __syncthreads();
+  // wavefront w ends rows of load n = w, w + 4, ...
+#pragma unroll
+  for (int n0 = 0; n0 < NR; n0 += WAVES) {
+    const int n = n0 + wave, row = row0 + n * RPI + sub;
+    if (n >= NR || row >= j.rows) continue;
+    float m = -INFINITY, l = 0.f, lr = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) m = fmaxf(m, part_s[k][n][sub][0]);
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) {
+      const f32x4 s = part_s[k][n][sub];
+      const float w = __builtin_amdgcn_exp2f(s[0] - ref);
+      l += s[1] * w;
+      lr += s[2] * w;
+      o += part_o[k][n][lane] * w;
+    }
+    const float inv = (l > 0.f && lr > 0.f) ? 1.f / lr : (l == l ? 0.f : l);   // (a row of NaN stays one)
+    const int i = token_of(c, j.row0 + row), head = j.h * c.G + (j.row0 + row) - i * c.G, token = j.first + i;
+    if (col == 0) c.LSE[(int64_t)head * c.b.T + token] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : (l == l ? -INFINITY : l);
+    if (col < c.d) {
+      typename Vec<T>::x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (T)(o[e] * inv);
+      *(typename Vec<T>::x4*)((T*)c.O + (int64_t)token * c.ot + (int64_t)head * c.oh + col) = v;
     }
   }
 }
@@ -181,12 +185,7 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
   __shared__ __attribute__((aligned(16))) T Ks[Shape::kStages][KEYS * D];
   __shared__ __attribute__((aligned(16))) T Vs[Shape::kStages][KEYS * D];
 
-  int slot;
-  Point at;
-  Sequence s;
-  int64_t x_end;
-  if (!stretch<Div>(c, slot, at, s, x_end)) return;
-
+  const Numbers numbers = Round::numbers(c, 0);   // (on their way while the lane's constants are made)
   const int lane = threadIdx.x, r = lane & 31, g = lane >> 5;
   const float cs = c.scale_log2;
   const int page_mask = (1 << c.b.page_log2) - 1;
@@ -204,10 +203,20 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
     for (int p = 0; p < COPIES; ++p)
       if (8 * ((lane % CPR) ^ swz_bits<D>(p * RPC + lane / CPR)) >= c.d) beyond |= 1u << p;
   }
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" ::"v"(tro.off[0][0]), "v"(goff[0]), "v"(goff[COPIES - 1]));
+#endif
 
+  Line<Div> line;
+  int slot;
+  Point at;
+  Sequence s;
+  double x_end;
+  if (!stretch<Div>(c, numbers, line, slot, at, s, x_end)) return;
+  bool first_item = true;
   while (true) {
-    const int64_t length = s.length(at.t);
-    const int64_t z1 = min(x_end - at.at, length);
+    const double length = s.length(at.t);
+    const double z1 = fmin(x_end - at.at, length);
     const int tiles = tiles_of<BR>(c, s, at.t, KEYS);
     const int j0 = cut_at(at.z, length, tiles), j1 = cut_at(z1, length, tiles);
     const int L = s.L;
@@ -217,17 +226,6 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
     const T* const Kg = (const T*)c.K + (int64_t)at.h * c.b.sh;
     const T* const Vg = (const T*)c.V + (int64_t)at.h * c.b.sh;
 
-    T8 qf[KK];
-    const T* const q_row = (const T*)c.Q + (int64_t)w.token * c.qt + (int64_t)w.head * c.qh;
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      if (D == 32 && 16 * kk + 8 * g >= c.d) {   // head dimension 16: the upper columns are zeros
-#pragma unroll
-        for (int e = 0; e < 8; ++e) qf[kk][e] = (T)0.f;
-      } else {
-        qf[kk] = *(const T8*)(q_row + 16 * kk + 8 * g);
-      }
-    }
     if (D == 32 && c.d < D) {   // (the copies leave columns >= 16 untouched, and O rows have stood there)
       zero_tiles(&Ks[0][0], Shape::kStages * KEYS * D);
       zero_tiles(&Vs[0][0], Shape::kStages * KEYS * D);
@@ -274,14 +272,23 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
       }
     };
 
-    if (j0 < j1) page_numbers(j0);
-    wait_async_copies();   // Q
+    T8 qf[KK];
+    const T* const q_row = (const T*)c.Q + (int64_t)w.token * c.qt + (int64_t)w.head * c.qh;
 #pragma unroll
-    for (int i = 0; i + 1 < STAGES; ++i)
-      if (j0 + i < j1) {
-        copy_tile(j0 + i, i);
-        if (j0 + i + 1 < j1) page_numbers(j0 + i + 1);
+    for (int kk = 0; kk < KK; ++kk) {
+      if (D == 32 && 16 * kk + 8 * g >= c.d) {   // head dimension 16: the upper columns are zeros
+#pragma unroll
+        for (int e = 0; e < 8; ++e) qf[kk][e] = (T)0.f;
+      } else {
+        qf[kk] = *(const T8*)(q_row + 16 * kk + 8 * g);
       }
+    }
+    if (j0 < j1) page_numbers(j0);
+    if (first_item) {   // (while Q and the page numbers are on their way)
+      leave_join<Div>(c, line, slot, at, s);
+      first_item = false;
+    }
+    wait_async_copies();   // Q (the compiler would wait for its loads, and all copies with them, in the loop)
     f32x16 o[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -289,16 +296,22 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
       for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
     float m_run = -INFINITY, l_run = 0.f, lr_run = 0.f;
 
-    int buf = 0;
-    for (int j = j0; j < j1; ++j) {
-      // tile j has landed, those behind it are on their way
-      if (STAGES > 2 && j + STAGES - 2 < j1) wait_async_copies_but<(STAGES - 2) * 2 * COPIES>();
-      else if (STAGES > 3 && j + 1 < j1) wait_async_copies_but<2 * COPIES>();
-      else wait_async_copies();
-      if (j + STAGES - 1 < j1) {   // into the buffer of tile j - 1, which this wavefront is done with
-        copy_tile(j + STAGES - 1, buf == 0 ? STAGES - 1 : buf - 1);
-        if (j + STAGES < j1) page_numbers(j + STAGES);
+    // Tile j is used while those behind it, up to j + STAGES - 1, are on their way.  (One place for the copies, also the first ones: short calls wait for instructions
+    // more than for anything else.)
+    int buf = 0, to = 0;
+#pragma clang loop unroll(disable)
+    for (int j = j0 - (STAGES - 1); j < j1; ++j) {
+      const int ahead = j + STAGES - 1;
+      if (ahead < j1) {   // into the buffer of tile j - 1, which this wavefront is done with
+        copy_tile(ahead, to);
+        to = to + 1 == STAGES ? 0 : to + 1;
+        if (ahead + 1 < j1) page_numbers(ahead + 1);
       }
+      if (j < j0) continue;
+      static_assert(STAGES == 3, "the waits below");
+      if (j + 2 < j1) wait_async_copies_but<2 * 2 * COPIES>();
+      else if (j + 1 < j1) wait_async_copies_but<2 * COPIES>();
+      else wait_async_copies();
       const T* const Kt = Ks[buf];
       const T* const Vt = Vs[buf];
       f32x16 st[NB];
@@ -324,10 +337,10 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
     }
 
     const float l_tot = l_run + xchg32(l_run), lr_sum = lr_run + xchg32(lr_run);
-    if (at.z == 0 && z1 == length) write_rows<T, D>(c, s, at.h, at.t * BR, o, m_run, l_tot, lr_sum, &Ks[0][0]);
-    else write_piece<D>(c, s, at.t, piece_index(slot, at.z == 0), o, m_run, l_tot, lr_sum);
-    const int64_t x = at.at + length;
-    if (x >= x_end || !next_item<BR>(c, x, at, s)) break;
+    if (at.z == 0.0 && z1 == length) write_rows<T, D>(c, s, at.h, at.t * BR, o, m_run, l_tot, lr_sum, &Ks[0][0]);
+    else write_piece<D>(c, s, at.t, piece_index(slot, at.z == 0.0), o, m_run, l_tot, lr_sum);
+    const double x = at.at + length;
+    if (x >= x_end || !next_item<Div>(c, x, at, s)) break;
   }
 }
 
@@ -335,7 +348,7 @@ template <typename T, int D> int launch(const PagedCall& c, hipStream_t s) {
   hipLaunchKernelGGL((paged_one_kernel<T, D>), dim3((c.slots + kXcds - 1) / kXcds * kXcds), dim3(64), 0, s, c);
   const int e = (int)hipGetLastError();
   if (e != 0) return e;
-  hipLaunchKernelGGL((paged_one_join_kernel<T, D>), dim3(c.slots - 1), dim3(1024), 0, s, c);
+  hipLaunchKernelGGL((paged_one_join_kernel<T, D>), dim3(c.slots - 1, 4), dim3(256), 0, s, c);
   return (int)hipGetLastError();
 }
 template <typename T> int launch_t(const PagedCall& c, hipStream_t s) {

@@ -12,7 +12,7 @@
 namespace attn {
 namespace {
 
-typedef Division<256, 256, 8> Div;
+typedef Division<256, 256, 64, 8> Div;
 constexpr int BR = Div::BR, BC = 64, NT = 512;
 
 // A piece in the layout of the accumulators: 16 bytes a lane at a time, whole lines; then the statistics of every wavefront's 32 rows.
@@ -82,11 +82,14 @@ __global__ __launch_bounds__(NT) void paged_rows_kernel(const PagedCall c) {
   __shared__ __attribute__((aligned(16))) T Ks[3][BC * D];
   __shared__ __attribute__((aligned(16))) T Vs[3][BC * D];
 
+  Line<Div> line;
   int slot;
   Point at;
   Sequence s;
-  int64_t x_end;
-  if (!stretch<Div>(c, slot, at, s, x_end)) return;
+  double x_end;
+  if (!stretch<Div>(c, Round::numbers(c, 0), line, slot, at, s, x_end)) return;
+  leave_join<Div>(c, line, slot, at, s);
+  if (!snap<Div>(c, line, slot, at, s, x_end)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool group_b = wave >= 4;
   const int part = wave & 3;   // rows 16 part .. + 15 of a tile are this wavefront's to copy
@@ -94,9 +97,9 @@ __global__ __launch_bounds__(NT) void paged_rows_kernel(const PagedCall c) {
   const int page_mask = (1 << c.b.page_log2) - 1;
 
   while (true) {
-    const int64_t length = s.length(at.t);
-    const int64_t z1 = min(x_end - at.at, length);
-    const bool whole = at.z == 0 && z1 == length;
+    const double length = s.length(at.t);
+    const double z1 = fmin(x_end - at.at, length);
+    const bool whole = at.z == 0.0 && z1 == length;
     const int tiles = tiles_of<BR>(c, s, at.t, BC);
     const int j0 = cut_at(at.z, length, tiles), J = cut_at(z1, length, tiles) - j0;   // tiles j0 .. j0 + J - 1
     const int L = s.L, row0 = at.t * BR + 32 * wave;
@@ -265,11 +268,11 @@ __global__ __launch_bounds__(NT) void paged_rows_kernel(const PagedCall c) {
         T* const stage = wave < 4 ? &Ks[0][0] + wave * 32 * D : &Vs[0][0] + (wave - 4) * 32 * D;
         write_rows<T, D>(c, s, at.h, row0, o, m_run, l_tot, lr_sum, stage);
       } else {
-        write_piece<D>(c, wave, piece_index(slot, at.z == 0), o, m_run, l_tot, lr_sum);
+        write_piece<D>(c, wave, piece_index(slot, at.z == 0.0), o, m_run, l_tot, lr_sum);
       }
     }
-    const int64_t x = at.at + length;
-    if (x >= x_end || !next_item<BR>(c, x, at, s)) break;
+    const double x = at.at + length;
+    if (x >= x_end || !next_item<Div>(c, x, at, s)) break;
     __syncthreads();   // the buffers are free again
   }
 }
