@@ -8,6 +8,8 @@
 //   A page holds 16 rows or more, so a tile has two page numbers at most, which scalar loads bring a tile ahead.
 #include "attn_paged_line.h"
 
+#include <algorithm>
+
 namespace attn {
 namespace {
 
@@ -85,16 +87,22 @@ __device__ __forceinline__ void write_piece(const PagedCall& c, const Sequence& 
   }
 }
 
-// Joins the pieces of the items that were cut: blockIdx.x + 1 is the slot of an item's first cut, blockIdx.y eight of its rows.  The four wavefronts take pieces by
-// fours in turn, 16 bytes of a row a lane, sixteen loads in flight, and meet in LDS.
-// us, the join alone: one piece after the other, rows in the accumulators' layout, 16 items of 16 pieces and 4 rows 98.6; 16 wavefronts an item, a row or a share of
-// one's pieces each, 48 pieces of 4 rows 13.8, but 8 items of 96 pieces and 16 rows about 50.
+// Joins the pieces of the items that were cut: blockIdx.x + 1 is the slot of an item's first cut, blockIdx.y four of its rows (eight at d <= 32).  The four wavefronts take
+// pieces by eights in turn, 16 bytes of a row a lane, all loads in flight together, and meet in LDS.
+// us, the join alone, two contexts of 10^5 tokens and 64 sequences (16 items of 48 pieces, about 400 of 2 or 3, 4 rows): this 7.6, 5.4; eight rows, pieces by fours 12.6, 6.7, with eight
+// wavefronts 9.5, 9.8.  (One piece after the other took 98.6 for 16 pieces; most of the grid has nothing to join, and large workgroups are slow to find that out.)
+template <int D> struct JoinShape {
+  static constexpr int kWaves = 4, kPieces = 8;                              // of a workgroup; pieces at a time
+  static constexpr int kLanes = D / 4, kRowsOfLoad = 64 / kLanes;            // lanes of a row
+  static constexpr int kLoads = kRowsOfLoad < 4 ? 4 / kRowsOfLoad : 1, kRows = kLoads * kRowsOfLoad;
+};
 template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_one_join_kernel(const PagedCall c) {
-  constexpr int WAVES = 4, LPR = D / 4, RPI = 64 / LPR, NR = 8 / RPI, NP = 4;   // lanes of a row, rows of a load, loads of a piece, pieces at a time
+__global__ __launch_bounds__(64 * JoinShape<D>::kWaves) void paged_one_join_kernel(const PagedCall c) {
+  typedef JoinShape<D> Shape;
+  constexpr int WAVES = Shape::kWaves, LPR = Shape::kLanes, RPI = Shape::kRowsOfLoad, NR = Shape::kLoads, NP = Shape::kPieces;
   __shared__ f32x4 part_o[WAVES][NR][64];
   __shared__ f32x4 part_s[WAVES][NR][RPI];
-  const int slot = (int)blockIdx.x + 1, row0 = 8 * (int)blockIdx.y;
+  const int slot = (int)blockIdx.x + 1, row0 = Shape::kRows * (int)blockIdx.y;
   const Join j = join_list(c)[slot];
   if (slot >= *join_slots(c) || j.pieces == 0 || row0 >= j.rows) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -348,7 +356,8 @@ template <typename T, int D> int launch(const PagedCall& c, hipStream_t s) {
   hipLaunchKernelGGL((paged_one_kernel<T, D>), dim3((c.slots + kXcds - 1) / kXcds * kXcds), dim3(64), 0, s, c);
   const int e = (int)hipGetLastError();
   if (e != 0) return e;
-  hipLaunchKernelGGL((paged_one_join_kernel<T, D>), dim3(c.slots - 1, 4), dim3(256), 0, s, c);
+  const int rows = c.b.starts ? BR : std::min(c.G, BR);   // of a block, at most
+  hipLaunchKernelGGL((paged_one_join_kernel<T, D>), dim3(c.slots - 1, (rows + JoinShape<D>::kRows - 1) / JoinShape<D>::kRows), dim3(64 * JoinShape<D>::kWaves), 0, s, c);
   return (int)hipGetLastError();
 }
 template <typename T> int launch_t(const PagedCall& c, hipStream_t s) {
