@@ -256,14 +256,14 @@ __device__ const u32x4 zero_line[1] = {{0u, 0u, 0u, 0u}};
 // this wavefront.  (Lane numbers that the compiler does not keep through the tile loop.)
 template <typename T, int D>
 __device__ __forceinline__ void write_rows(const PagedCall& c, const Sequence& s, int h, int row0, const f32x16 (&o)[D / 32], float m_run, float l_tot, float lr_sum,
-                                           T* stage) {
+                                           T* stage, bool with_lse = true) {
   typedef typename Vec<T>::x4 T4;
   typedef typename Vec<T>::x8 T8;
   constexpr int CPR = D / 8, RPP = 64 / CPR;
   const int lane = lane_id_here(), r = lane & 31, g = lane >> 5;
   const Rows w = rows_of(c, s, h, row0, r);
   const float inv = (l_tot > 0.f && lr_sum > 0.f) ? 1.f / lr_sum : (l_tot == l_tot ? 0.f : l_tot);   // (a row of NaN stays one)
-  if (g == 0 && w.ok)
+  if (with_lse && g == 0 && w.ok)
     c.LSE[(int64_t)w.head * c.b.T + w.token] =
         l_tot > 0.f ? (m_run + __builtin_amdgcn_logf(l_tot)) * 0.6931471805599453f : (l_tot == l_tot ? -INFINITY : l_tot);
 #pragma unroll

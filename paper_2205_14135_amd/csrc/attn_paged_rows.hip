@@ -35,44 +35,58 @@ template <int D> __device__ __forceinline__ void write_piece(const PagedCall& c,
   }
 }
 
-// Joins the pieces of the items that were cut: blockIdx.x + 1 is the slot of an item's first cut; a wavefront does 32 rows.  (Rows one after the other, and lanes as
-// columns, as for single tokens: chunk of 2048 tokens on 14336, two or three pieces of most of 256 items, 32 us.)
+// Joins the pieces of the items that were cut: blockIdx.x + 1 is the slot of an item's first cut, blockIdx.y 32 columns; a wavefront does 32 rows, four pieces at a time.
+// (Rows one after the other, and lanes as columns, as for single tokens: chunk of 2048 tokens on 14336, two or three pieces of most of 256 items, 32 us; all columns by one
+// wavefront, a piece at a time, 14.6.)
 template <typename T, int D>
 __global__ __launch_bounds__(NT) void paged_rows_join_kernel(const PagedCall c) {
-  constexpr int DB = D / 32;
-  __shared__ __attribute__((aligned(16))) T stage[NT / 64][32 * D];
-  const int slot = (int)blockIdx.x + 1;
+  constexpr int NP = 4;
+  __shared__ __attribute__((aligned(16))) T stage[NT / 64][32 * 32];
+  const int slot = (int)blockIdx.x + 1, db = (int)blockIdx.y;
   const Join j = join_list(c)[slot];
   if (slot >= *join_slots(c) || j.pieces == 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (32 * wave >= j.rows) return;
-  f32x16 o[DB];
+  f32x16 o[1];
 #pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  for (int i = 0; i < 16; ++i) o[0][i] = 0.f;
   float m = -INFINITY, l = 0.f, lr = 0.f;
-  for (int k = 0; k < j.pieces; ++k) {
-    float* const piece = piece_of<D, BR>(c, piece_index(slot - 1 + k, k == 0));
-    const f32x4* const po = piece_o<D>(piece, wave, lane);
-    const f32x4 st = *piece_s<D>(piece, wave, lane);
-    f32x4 v[4 * DB];
+  for (int k0 = 0; k0 < j.pieces; k0 += NP) {
+    f32x4 st[NP], v[NP][4];
 #pragma unroll
-    for (int i = 0; i < 4 * DB; ++i) v[i] = po[64 * i];
-    const float top = fmaxf(m, st[0]), ref = top == -INFINITY ? 0.f : top;
-    const float w0 = __builtin_amdgcn_exp2f(m - ref), w1 = __builtin_amdgcn_exp2f(st[0] - ref);
+    for (int i = 0; i < NP; ++i) {
+      const int k = min(k0 + i, j.pieces - 1);
+      float* const piece = piece_of<D, BR>(c, piece_index(slot - 1 + k, k == 0));
+      const f32x4* const po = piece_o<D>(piece, wave, lane) + 256 * db;
+      st[i] = *piece_s<D>(piece, wave, lane);
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) v[i][i4] = po[64 * i4];
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) top = fmaxf(top, st[i][0]);   // (the last piece more than once: no harm)
+    const float ref = top == -INFINITY ? 0.f : top, w0 = __builtin_amdgcn_exp2f(m - ref);
     m = top;
-    l = l * w0 + st[1] * w1;
-    lr = lr * w0 + st[2] * w1;
+    l *= w0;
+    lr *= w0;
 #pragma unroll
-    for (int i = 0; i < 4 * DB; ++i)
+    for (int e = 0; e < 16; ++e) o[0][e] *= w0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[i / 4][4 * (i % 4) + e] = o[i / 4][4 * (i % 4) + e] * w0 + v[i][e] * w1;
+    for (int i = 0; i < NP; ++i) {
+      if (k0 + i >= j.pieces) break;
+      const float w = __builtin_amdgcn_exp2f(st[i][0] - ref);
+      l += st[i][1] * w;
+      lr += st[i][2] * w;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[0][e] += v[i][e / 4][e % 4] * w;
+    }
   }
   Sequence s = {};
   s.first = j.first;
   s.rows = j.row0 + j.rows;   // (of the item's sequence, as far as this block goes)
-  write_rows<T, D>(c, s, j.h, j.row0 + 32 * wave, o, m, l, lr, stage[wave]);
+  PagedCall slice = c;
+  slice.O = (T*)c.O + 32 * db;
+  write_rows<T, 32>(slice, s, j.h, j.row0 + 32 * wave, o, m, l, lr, stage[wave], db == 0);
 }
 
 template <typename T, int D>
@@ -140,6 +154,9 @@ __global__ __launch_bounds__(NT) void paged_rows_kernel(const PagedCall c) {
         if ((j & ~15) != window) {
           window = j & ~15;
           ids = ids_next;
+#if defined(__HIP_DEVICE_COMPILE__)
+          asm volatile("" : "+v"(ids));   // (arrived from here on: else every tile waits for what might be its load, and for the copies behind that)
+#endif
           ids_next = page_numbers(window + 16);
         }
         const int id = __builtin_amdgcn_readlane(ids, 4 * (j & 15) + part);
@@ -281,7 +298,7 @@ template <typename T, int D> int launch(const PagedCall& c, hipStream_t s) {
   hipLaunchKernelGGL((paged_rows_kernel<T, D>), dim3(c.slots), dim3(NT), 0, s, c);
   const int e = (int)hipGetLastError();
   if (e != 0) return e;
-  hipLaunchKernelGGL((paged_rows_join_kernel<T, D>), dim3(c.slots - 1), dim3(NT), 0, s, c);
+  hipLaunchKernelGGL((paged_rows_join_kernel<T, D>), dim3(c.slots - 1, D / 32), dim3(NT), 0, s, c);
   return (int)hipGetLastError();
 }
 template <typename T> int launch_t(const PagedCall& c, hipStream_t s) {
