@@ -11,12 +11,13 @@
 
 namespace attn {
 
-// How a kernel divides its line: rows of a block, what an item costs beside its keys, in keys (Q, the wait for its first tile, its end), keys of a stretch at
-// least, and the share of a stretch (0: none) that a cut is moved by to an item's end.
-template <int BR_, int ITEM_, int LEAST_, int SLACK_> struct Division {
-  static constexpr int BR = BR_, ITEM = ITEM_, LEAST = LEAST_, SLACK = SLACK_;
+// How a kernel divides its line.  BR: rows of a block.  KEYS: of a tile.  ITEM: what an item costs beside its keys, in keys (Q, the wait for its first tile, its end); a piece costs
+// as much, and a join.  SPREAD: a stretch has at least the square root of SPREAD times the longest item's keys, so that joining the pieces takes no longer than making one:
+// with k keys in each of n / k pieces the kernel takes c k for a piece, the join C n / k, and the sum is least at k^2 = n C / c.
+template <int BR_, int KEYS_, int ITEM_, int SPREAD_> struct Division {
+  static constexpr int BR = BR_, KEYS = KEYS_, ITEM = ITEM_, SPREAD = SPREAD_;
+  static constexpr int SLACK = (ITEM + KEYS) / 2;   // keys that a cut is moved by to an end of its item: an item of one tile is never cut
 };
-
 // A sequence of the batch, every number taken from device memory forced into its range.
 struct Sequence {
   int first;   // its first token's row of Q
@@ -77,15 +78,17 @@ struct Point {
 // 64 sequences of the line, one a lane: its stretch, and the sum up to its end.
 struct Round {
   Sequence s;
-  double cost, incl;
+  double cost, incl, longest;   // longest: of the items of all 64
   static __device__ __forceinline__ Numbers numbers(const PagedCall& c, int b0) { return Numbers(c, min(b0 + (int)(threadIdx.x & 63), c.b.B - 1)); }
   template <class DIV> __device__ __forceinline__ void load(const PagedCall& c, int b0, const Numbers& numbers) {
     const int lane = threadIdx.x & 63, n = c.b.B - b0;
     s = load_sequence<DIV>(c, numbers);
     cost = lane < n ? s.upto(s.blocks) * c.b.Hk : 0.0;
     incl = cost;
+    longest = s.blocks > 0 ? s.length(s.blocks - 1) : 0.0;
     for (int d = 1; d < min(n, 64); d <<= 1) {
       const double other = __shfl_up(incl, d, 64);
+      longest = fmax(longest, __shfl_xor(longest, d, 64));
       if (lane >= d) incl += other;
     }
   }
@@ -97,21 +100,25 @@ template <class DIV> struct Line {
   Round first;      // all there is for up to 64 sequences
   int n;            // slots that get a stretch
   double each;      // its length, not a whole number
-  double slack;     // a cut nearer than this to an item's end is made there
+  double slack;     // a cut no farther than this from an item's start, or else from its end, is made there
 
   __device__ __forceinline__ void init(const PagedCall& c, const Numbers& numbers) {
     first.load<DIV>(c, 0, numbers);
     total = lane_double(first.incl, min(c.b.B, 64) - 1);
+    double longest = lane_double(first.longest, 0);
 #pragma clang loop unroll(disable)
     for (int b0 = 64; b0 < c.b.B; b0 += 64) {
       Round r;
       r.load<DIV>(c, b0, Round::numbers(c, b0));
       total += lane_double(r.incl, min(c.b.B - b0, 64) - 1);
+      longest = fmax(longest, lane_double(r.longest, 0));
     }
-    const double worth = total / ((double)(DIV::LEAST + DIV::ITEM) * c.G);
-    n = __builtin_amdgcn_readfirstlane((int)fmin(fmax(worth, 1.0), (double)c.slots));
+    // (with stretches no longer than an item without keys, every end of an item has a cut near it)
+    const float item = (float)longest / (float)c.G;   // in keys
+    const float least = fmaxf((float)DIV::ITEM, sqrtf((float)DIV::SPREAD * item));
+    n = __builtin_amdgcn_readfirstlane((int)fmin(fmax(total / ((double)least * c.G), 1.0), (double)c.slots));
     each = total / n;
-    slack = DIV::SLACK > 0 ? floor(each / (DIV::SLACK > 0 ? DIV::SLACK : 1)) : 0.0;
+    slack = (double)DIV::SLACK * c.G;
   }
   __device__ __forceinline__ double start(int slot) const { return slot < n ? floor(each * slot) : total; }   // (each * slot < total: grows with the slot)
   // The item at 0 <= x < total, and its sequence.
@@ -201,19 +208,18 @@ template <class DIV> __device__ __forceinline__ void leave_join(const PagedCall&
     join_list(c)[slot] = j;
   }
 }
-// Moves the cuts of a stretch that are near an item's end there.  False: nothing is left.
-template <class DIV> __device__ __forceinline__ bool snap(const PagedCall& c, const Line<DIV>& line, int slot, Point& at, Sequence& s, double& x_end) {
-  if (slot + 1 < line.n) {
-    Sequence last;
-    const Point e = line.locate(c, x_end, last);
-    const double v = last.length(e.t);
-    if (e.z <= line.slack) x_end = e.at;
-    else if (v - e.z <= line.slack) x_end = e.at + v;
-  }
+// Moves a cut at the start of a stretch.  False: there is nothing behind it.
+template <class DIV> __device__ __forceinline__ bool from_here(const PagedCall& c, const Line<DIV>& line, Point& at, Sequence& s) {
   const double v = s.length(at.t);
   if (at.z <= line.slack) at.z = 0.0;
   else if (v - at.z <= line.slack) return next_item<DIV>(c, at.at + v, at, s);
   return true;
+}
+// Where a stretch that ends at x_end on the line ends in the item at `at`, v long: 0 in front of it, v at its end or behind.
+template <class DIV> __device__ __forceinline__ double up_to_here(const Line<DIV>& line, int slot, const Point& at, double v, double x_end) {
+  const double z1 = x_end - at.at;
+  if (slot + 1 < line.n && z1 <= line.slack) return 0.0;
+  return v - z1 <= line.slack ? v : z1;
 }
 
 // row / G

@@ -13,7 +13,7 @@
 namespace attn {
 namespace {
 
-typedef Division<32, 64, 64, 0> Div;
+typedef Division<32, 32, 64, 1> Div;
 constexpr int BR = Div::BR;
 
 // (us, the main kernel.  d = 64, tiles of 64 keys | 32: one token over 777 keys 9.5 | 7.6, 32 sequences of up to 2000 35.9 | 35.1 with the join.  d = 128, 64 sequences and two contexts of
@@ -221,10 +221,12 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
   Sequence s;
   double x_end;
   if (!stretch<Div>(c, numbers, line, slot, at, s, x_end)) return;
-  bool first_item = true;
+  leave_join<Div>(c, line, slot, at, s);
+  if (!from_here<Div>(c, line, at, s)) return;
   while (true) {
     const double length = s.length(at.t);
-    const double z1 = fmin(x_end - at.at, length);
+    const double z1 = up_to_here(line, slot, at, length, x_end);
+    if (z1 == 0.0) break;
     const int tiles = tiles_of<BR>(c, s, at.t, KEYS);
     const int j0 = cut_at(at.z, length, tiles), j1 = cut_at(z1, length, tiles);
     const int L = s.L;
@@ -292,10 +294,6 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
       }
     }
     if (j0 < j1) page_numbers(j0);
-    if (first_item) {   // (while Q and the page numbers are on their way)
-      leave_join<Div>(c, line, slot, at, s);
-      first_item = false;
-    }
     wait_async_copies();   // Q (the compiler would wait for its loads, and all copies with them, in the loop)
     f32x16 o[DB];
 #pragma unroll

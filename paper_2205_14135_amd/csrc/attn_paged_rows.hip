@@ -12,7 +12,7 @@
 namespace attn {
 namespace {
 
-typedef Division<256, 256, 64, 8> Div;
+typedef Division<256, 64, 256, 18> Div;
 constexpr int BR = Div::BR, BC = 64, NT = 512;
 
 // A piece in the layout of the accumulators: 16 bytes a lane at a time, whole lines; then the statistics of every wavefront's 32 rows.
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(NT) void paged_rows_kernel(const PagedCall c) {
   double x_end;
   if (!stretch<Div>(c, Round::numbers(c, 0), line, slot, at, s, x_end)) return;
   leave_join<Div>(c, line, slot, at, s);
-  if (!snap<Div>(c, line, slot, at, s, x_end)) return;
+  if (!from_here<Div>(c, line, at, s)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool group_b = wave >= 4;
   const int part = wave & 3;   // rows 16 part .. + 15 of a tile are this wavefront's to copy
@@ -112,7 +112,8 @@ __global__ __launch_bounds__(NT) void paged_rows_kernel(const PagedCall c) {
 
   while (true) {
     const double length = s.length(at.t);
-    const double z1 = fmin(x_end - at.at, length);
+    const double z1 = up_to_here(line, slot, at, length, x_end);
+    if (z1 == 0.0) break;
     const bool whole = at.z == 0.0 && z1 == length;
     const int tiles = tiles_of<BR>(c, s, at.t, BC);
     const int j0 = cut_at(at.z, length, tiles), J = cut_at(z1, length, tiles) - j0;   // tiles j0 .. j0 + J - 1
