@@ -184,3 +184,65 @@ def test_prompt_fork_and_single_tokens_together(d, Hq, Hk, interleaved):
     u = 2.0 ** -8
     assert (got.float() - want.float()).abs().max().item() <= 2 * (2 * u * 12 + 6 * u)
     assert (got.float() - want.float()).pow(2).mean().sqrt().item() <= 2 * u     # (rms of values below 1: two roundings of each)
+
+
+def test_sequences_forked_ended_and_compacted():
+    """Three prompts in a cache of two layers through `PageTable`: forked, continued apart, one ended, the cache compacted, continued; every step's attention against the same
+    in 64 bits over all tokens that the sequence was given (turned and rounded as the cache holds them)."""
+    from paper_2205_14135_amd.paged import PageTable
+    Hq, Hk, d, page, layers = 4, 2, 64, 16, 2
+    gen = torch.Generator().manual_seed(3)
+    table = PageTable(30, page)
+    kc, vc = (torch.full((layers, table.pages, Hk, page, d), math.nan, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    given = {}      # sequence -> per layer, K and V rows on the CPU
+
+    def step(seqs, new):
+        pairs = table.extend(seqs, new)
+        binding.attn_paged_copy(kc, vc, pairs)
+        block, lengths = table.batch(seqs)
+        starts = torch.tensor([sum(new[:i]) for i in range(len(new) + 1)], dtype=torch.int32, device="cuda")
+        T = sum(new)
+        for l in range(layers):
+            q, k, v = (torch.randn(T, h, d, generator=gen).to(torch.bfloat16) for h in (Hq, Hk, Hk))
+            binding.attn_paged_append(k.cuda(), v.cuda(), kc[l], vc[l], block, lengths, starts)
+            out, lse = binding.attn_paged_fwd(q.cuda(), kc[l], vc[l], block, lengths, starts, softmax_scale=d ** -0.5)
+            at = 0
+            for s, n in zip(seqs, new):
+                given[s][l][0].append(k[at:at + n])
+                given[s][l][1].append(v[at:at + n])
+                at += n
+            # the same batch on plain rows: pages in order
+            plain = ph.Batch([table.length(s) - n for s, n in zip(seqs, new)], new, Hq, Hk, d, "bf16", page)
+            plain.q = q
+            for cache, i in ((plain.kc, 0), (plain.vc, 1)):
+                for b, s in enumerate(seqs):
+                    rows = torch.cat(given[s][l][i])
+                    for t in range(-(-len(rows) // page)):
+                        part = rows[t * page:(t + 1) * page]
+                        cache[int(plain.table[b, t]), :, :len(part)] = part.transpose(0, 1)
+            want, want_l, bound, bound_l = ph.attention(plain, True)
+            ph.assert_within(out, want, bound, "O")
+            ph.assert_within(lse, want_l, bound_l, "LSE")
+
+    def fork(s):
+        t = table.fork(s)
+        given[t] = [[list(x) for x in layer] for layer in given[s]]
+        return t
+
+    a, b, c = (table.add() for _ in range(3))
+    for s in (a, b, c):
+        given[s] = [[[], []] for _ in range(layers)]
+    step([a, b, c], [37, 5, 64])
+    e, f = fork(a), fork(c)
+    step([e, a, f], [3, 1, 2])
+    step([b, c, e], [1, 1, 20])
+    table.free(a)
+    table.free(f)
+    pairs = table.compact()
+    assert pairs
+    binding.attn_paged_copy(kc, vc, pairs)
+    kc[:, table.pages - table.free_pages:] = math.nan
+    vc[:, table.pages - table.free_pages:] = math.nan
+    step([e, b, c], [1, 1, 1])
+    g = fork(e)
+    step([g, e, b, c], [1, 1, 30, 1])
