@@ -361,7 +361,8 @@ typedef struct {
 int attn_paged_append(const attn_paged_params* p, const attn_rotary_spec* rotary, const void* K, const void* V, void* k_cache, void* v_cache, const void* Q,
                       void* Qout);
 
-/* Bytes of scratch for attn_paged_fwd with these params (B, T, Hq, Hk, d decide).  0 if the params are invalid. */
+/* Bytes of scratch for attn_paged_fwd with these params.  The head dimension alone decides: a workspace serves every call at its head dimension.  0 if the params
+ * are invalid. */
 size_t attn_paged_workspace_bytes(const attn_paged_params* p);
 
 /*

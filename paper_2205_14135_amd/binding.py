@@ -340,8 +340,8 @@ def attn_paged_append(K, V, k_cache, v_cache, block_table, lengths, query_starts
 
 
 def attn_paged_workspace(Q, k_cache, sequences: int) -> torch.Tensor:
-    """A workspace for attn_paged_fwd with these sizes, on the device of Q.  Calls that may overlap in time (other streams, captured graphs that are replayed side by
-    side) need one each.  One made for more than 32 rows (tokens times the Q heads of a K head) a sequence serves fewer rows, too, at the same head dimension."""
+    """A workspace for attn_paged_fwd, on the device of Q; one serves every call at the same head dimension, one after the other.  Calls that may overlap in time (on
+    other streams, in captured graphs that are replayed side by side) need one each."""
     if _lib is None:
         load()
     n = _marshal.paged_workspace_bytes(Q, k_cache, sequences)

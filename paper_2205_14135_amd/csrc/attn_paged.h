@@ -76,22 +76,24 @@ struct PagedCall {
 // How attn_paged_fwd runs: blocks of 32 rows, a wavefront each (attn_paged_one.hip), or of 256 (attn_paged_rows.hip), and the workgroups that share the work.
 struct PagedShape { int rows, slots; };
 int paged_one_slots(int d);
+int paged_rows_slots(int d);
 // Blocks of 32 rows where a sequence has no more on average (single tokens), or where all blocks together are few, so that their keys are divided over many workgroups:
 // pieces of 32 rows are joined sooner than pieces of 256.  Else a block of 256 rows uses a tile of K and V eight times as often.  us, 32 | 256, sequences x new tokens on
 // tokens before: d = 128, 32 / 8 heads 1 x 32 on 16000 (32 blocks of 32 rows) 53 | 65, 1 x 64 on 2000 (64) 29 | 39, on 16000 83 | 76, 1 x 128 on 2000 (128) 38 | 44, on 16000 145 | 76, 8 x 16 on
 // 2000 (128) 37 | 29, 32 x 4 on 2000 (a block a sequence) 53 | 53; d = 64, 16 / 4 heads 1 x 128 on 16000 (64) 48 | 68, 8 x 32 on 2000 (128) 23 | 30, on 16000 79 | 55, 8 x 128 on 2000 52 | 35.
 inline PagedShape paged_shape(int64_t rows, int B, int Hk, int d) {
-#ifdef V_FORCE
-  if (V_FORCE == 32) return {32, paged_one_slots(d)};
-#else
   if (rows <= (int64_t)32 * B || Hk * ((rows + 31) / 32 + B - 1) <= 64) return {32, paged_one_slots(d)};
-#endif
-  return {256, kComputeUnits * (d == 128 ? 1 : (d == 64 ? 1 : 2))};
+  return {256, paged_rows_slots(d)};
 }
-// The number of slots and what to join at each of them (Join in attn_paged_line.h), then two pieces a slot: 32-bit rows of O and three statistics (Piece).
+// The number of slots and what to join at each of them (Join in attn_paged_line.h), then two pieces a slot: 32-bit rows of O and three statistics.  Room for either
+// kernel, so that a workspace serves every call at its head dimension.
 constexpr int kJoinBytes = 32;
 inline size_t paged_part_bytes(const PagedShape& s, int d) {
   return (size_t)(s.slots + 1) * kJoinBytes + (size_t)2 * s.slots * s.rows * ((d <= 32 ? 32 : d) + 4) * sizeof(float);
+}
+inline size_t paged_workspace_bytes(int d) {
+  const size_t one = paged_part_bytes({32, paged_one_slots(d)}, d), rows = paged_part_bytes({256, paged_rows_slots(d)}, d);
+  return one > rows ? one : rows;
 }
 
 int launch_rotary(const RotaryCall& c, int dtype, hipStream_t s);

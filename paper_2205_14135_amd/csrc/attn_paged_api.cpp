@@ -64,7 +64,7 @@ int check_batch(const attn_paged_params* p, attn::PagedBatch* out) {
   if (!dtype_ok(p->dtype)) return ATTN_ERR_DTYPE;
   if (!head_dim_ok(p->d)) return ATTN_ERR_HEADDIM;
   if (p->B <= 0 || p->T <= 0 || p->Hq <= 0 || p->Hk <= 0 || p->Hq % p->Hk != 0 || p->table_width <= 0) return ATTN_ERR_SHAPE;
-  if (p->B > (1 << 24) || p->T > (1 << 28) || p->Hq > (1 << 16) || (int64_t)p->T * p->Hq > (int64_t)1 << 30) return ATTN_ERR_SHAPE;
+  if (p->B > (1 << 20) || p->T > (1 << 28) || p->Hq > (1 << 16) || (int64_t)p->T * p->Hq > (int64_t)1 << 30) return ATTN_ERR_SHAPE;
   const int st = check_caches(p->pages, p->Hk, p->page_size, p->d, p->page_stride, p->head_stride, p->row_stride);
   if (st != ATTN_OK) return st;
   if ((int64_t)p->table_width * p->page_size > (int64_t)1 << 30) return ATTN_ERR_SHAPE;
@@ -177,7 +177,7 @@ int attn_paged_append(const attn_paged_params* p, const attn_rotary_spec* rotary
 size_t attn_paged_workspace_bytes(const attn_paged_params* p) {
   attn::PagedCall c;
   attn::PagedShape shape;
-  return check_paged(p, &c, &shape) == ATTN_OK ? attn::paged_part_bytes(shape, p->d) : 0;
+  return check_paged(p, &c, &shape) == ATTN_OK ? attn::paged_workspace_bytes(p->d) : 0;
 }
 
 int attn_paged_fwd(const attn_paged_params* p, const void* Q, const void* k_cache, const void* v_cache, void* O, float* LSE, void* workspace,
@@ -192,7 +192,7 @@ int attn_paged_fwd(const attn_paged_params* p, const void* Q, const void* k_cach
   for (const void* q : {Q, k_cache, v_cache, (const void*)O})
     if (!aligned(q, 16)) return ATTN_ERR_SHAPE;
   if (!aligned(LSE, 4)) return ATTN_ERR_SHAPE;
-  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < attn::paged_part_bytes(shape, p->d)) return ATTN_ERR_WORKSPACE;
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < attn::paged_workspace_bytes(p->d)) return ATTN_ERR_WORKSPACE;
   c.Q = Q; c.K = k_cache; c.V = v_cache; c.O = O; c.LSE = LSE;
   c.part = (float*)workspace;
   const int e = shape.rows == 32 ? attn::launch_paged_one(c, p->dtype, (hipStream_t)p->stream) : attn::launch_paged_rows(c, p->dtype, (hipStream_t)p->stream);

@@ -310,6 +310,8 @@ template <typename T> int launch_t(const PagedCall& c, hipStream_t s) {
 
 }  // namespace
 
+// Workgroups that the chip holds: two wavefronts a SIMD each, and at d <= 32 registers for twice as many.
+int paged_rows_slots(int d) { return kComputeUnits * (d <= 32 ? 2 : 1); }
 int launch_paged_rows(const PagedCall& c, int dtype, hipStream_t s) { return dtype == ATTN_FP16 ? launch_t<_Float16>(c, s) : launch_t<__bf16>(c, s); }
 
 }  // namespace attn

@@ -70,6 +70,31 @@ def test_many_sequences(B, single):
     check(ph.Batch([(b * 37) % 150 for b in range(B)], new, 2, 1, 64, "bf16", 16, seed=B), single=single)
 
 
+@pytest.mark.parametrize("single", [True, False])
+def test_very_many_sequences(single):
+    B = 1500
+    check(ph.Batch([(b * 37) % 70 for b in range(B)], [1] * B if single else [(b * 7) % 3 for b in range(B)], 2, 1, 32, "bf16", 16, pad=0 if single else 5, seed=4), single=single)
+
+
+def test_single_tokens_of_a_padded_batch():
+    """More rows of Q than sequences: those behind are left as they were."""
+    check(ph.Batch([30, 400, 7], [1, 1, 1], 8, 2, 64, "bf16", 16, pad=5, seed=40), single=True)
+
+
+def test_rows_in_front_of_the_first_sequence_and_a_part_of_a_table():
+    batch = ph.Batch([30, 400], [3, 70], 8, 2, 64, "bf16", 16, seed=41)
+    q, kc, vc, table, lengths, starts = batch.gpu()
+    q = torch.cat([torch.full((4, 8, 64), math.nan, dtype=q.dtype, device="cuda"), q])
+    wide = torch.full((2, table.shape[1] + 9), 10 ** 9, dtype=torch.int32, device="cuda")
+    wide[:, 3:3 + table.shape[1]] = table
+    out, lse = torch.full_like(q, 7.0), torch.full((8, q.shape[0]), 5.0, device="cuda")
+    binding.attn_paged_fwd(q, kc, vc, wide[:, 3:3 + table.shape[1]], lengths, starts + 4, softmax_scale=batch.tau, out=out, lse=lse)
+    want, want_l, bound, bound_l = ph.attention(batch, True)
+    ph.assert_within(out[4:], want, bound, "O")
+    ph.assert_within(lse[:, 4:], want_l, bound_l, "LSE")
+    assert (out[:4] == 7.0).all() and (lse[:, :4] == 5.0).all()
+
+
 @pytest.mark.parametrize("d", [16, 128])
 @pytest.mark.parametrize("causal", [True, False])
 def test_rows_that_see_nothing(d, causal):
@@ -215,5 +240,76 @@ def test_two_streams_with_workspaces_of_their_own():
             with torch.cuda.stream(s):
                 got[i] = binding.attn_paged_fwd(*args[i], softmax_scale=batches[0].tau)
     torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])
+
+
+def test_graphs_of_whole_steps_share_a_workspace():
+    """Two captured steps, appending and attending, of one token a sequence: the lengths count on inside the graph; replayed in turn on one workspace, against eager steps
+    of the same tokens on a second cache."""
+    from paper_2205_14135_amd.rotary import Rotary
+    Hq, Hk, d, page, B, before = 8, 2, 64, 16, 3, 600
+    rotary = Rotary.make(d)
+    gen = torch.Generator(device="cuda").manual_seed(50)
+    normal = lambda *shape: torch.randn(shape, generator=gen, device="cuda").to(torch.bfloat16)
+    pages = B * 48
+    caches = [[normal(pages, Hk, page, d) for _ in range(2)] for _ in range(2)]          # of the two graphs
+    eager = [[c.clone() for c in pair] for pair in caches]
+    table = torch.randperm(pages, generator=gen, device="cuda").to(torch.int32).view(B, 48)
+    q, k, v = normal(B, Hq, d), normal(B, Hk, d), normal(B, Hk, d)
+    ws = binding.attn_paged_workspace(q, caches[0][0], B)
+    lengths = [torch.tensor([before, before + 5, 3], dtype=torch.int32, device="cuda") for _ in range(2)]
+    outs = [(torch.zeros_like(q), torch.zeros(Hq, B, device="cuda"), torch.zeros_like(q)) for _ in range(2)]
+
+    def step(pair, n, out, lse, turned):
+        binding.attn_paged_append(k, v, *pair, table, n, Q=q, rotary=rotary, out=turned)
+        binding.attn_paged_fwd(turned, *pair, table, n, softmax_scale=d ** -0.5, out=out, lse=lse, workspace=ws)
+
+    graphs = []
+    for i in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            lengths[i] += 1
+            step(caches[i], lengths[i], *outs[i])
+        graphs.append(graph)
+    seen = [n.clone() for n in lengths]
+    for rep in range(4):
+        for i in range(2):
+            for x in (q, k, v):
+                x.copy_(normal(*x.shape))
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            got = [x.clone() for x in outs[i]]
+            seen[i] += 1
+            want = tuple(torch.zeros_like(x) for x in outs[i])
+            step(eager[i], seen[i], *want)
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want)), (rep, i)
+            assert all(torch.equal(a, b) for a, b in zip(caches[i], eager[i]))
+
+
+def test_two_host_threads():
+    import threading
+    batches = [ph.Batch([2000 + i, 40], [1, 60], 8, 2, 64, "bf16", 16, seed=60 + i) for i in range(2)]
+    args = [b.gpu() for b in batches]
+    want = [binding.attn_paged_fwd(*a, softmax_scale=batches[0].tau) for a in args]
+    torch.cuda.synchronize()
+    got, errors = [None, None], []
+
+    def worker(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    got[i] = binding.attn_paged_fwd(*args[i], softmax_scale=batches[0].tau)
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=worker, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
     for g, w in zip(got, want):
         assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])

@@ -122,9 +122,9 @@ def test_paged_fwd_pointers_and_workspace(lib):
     assert lib.attn_paged_fwd(ctypes.byref(p), *[OK_PTR] * 5, ctypes.c_void_p(0x10010), need) == -7
     assert lib.attn_paged_fwd(ctypes.byref(p), *[OK_PTR] * 5, OK_PTR, need - 1) == -7
     assert lib.attn_paged_fwd(None, *[OK_PTR] * 5, OK_PTR, need) == -1
-    # one made for chunks serves single tokens
-    chunk = _paged(T=1000, query_starts=0x50000)
-    assert lib.attn_paged_workspace_bytes(ctypes.byref(chunk)) >= need
+    # one serves every call at its head dimension
+    assert lib.attn_paged_workspace_bytes(ctypes.byref(_paged(T=1000, query_starts=0x50000))) == need
+    assert lib.attn_paged_workspace_bytes(ctypes.byref(_paged(B=60, T=60, Hq=4, causal=1))) == need
 
 
 def _append(lib, p, rotary=True, spec=None, args=None):
