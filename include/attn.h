@@ -324,7 +324,8 @@ int attn_rotary(const attn_rotary_params* p, const attn_rotary_tensor* tensors, 
 
 /*
  * A batch of B sequences whose keys and values lie in the pages of a cache.
- *   caches         K and V: [pages, Hk, page_size, d], strides shared by both (multiples of 8 elements, d contiguous)
+ *   caches         K and V: [pages, Hk, page_size, d], strides shared by both (multiples of 8 elements, d contiguous); page_stride and
+ *                  row_stride * page_size below 2^31 elements
  *   block_table    device int32 [B, table_width]: entry t of row b is the page of positions t * page_size ...
  *   lengths        device int32 [B]: tokens of each sequence, the new ones included
  *   query_starts   device int32 [B + 1], rising: rows query_starts[b] .. query_starts[b + 1] - 1 of the token tensors [T, heads, d] are the

@@ -46,6 +46,7 @@ struct PagedBatch {
   int pages, page_log2, width;
   int capacity;           // width << page_log2: tokens that a row of the table holds
   int64_t sp, sh, sn;     // strides of the caches: page, head, row
+  uint32_t page_bytes, row_bytes, page_mask;   // sp and sn in bytes; rows of a page - 1
 };
 
 struct AppendCall {
@@ -73,17 +74,20 @@ struct PagedCall {
   float scale_log2;       // tau * log2(e)
 };
 
-// How attn_paged_fwd runs: blocks of 32 rows, a wavefront each (attn_paged_one.hip), or of 256 (attn_paged_rows.hip), and the workgroups that share the work.
+// How attn_paged_fwd runs: blocks of 32 rows, a wavefront each (attn_paged_one.hip), or of 128 or 256 (attn_paged_rows.hip), and the workgroups that share the work.
 struct PagedShape { int rows, slots; };
 int paged_one_slots(int d);
 int paged_rows_slots(int d);
+// rows of the larger blocks (attn_paged_rows.hip)
+constexpr int paged_block_rows(int d) { return d == 128 ? 256 : 128; }
 // Blocks of 32 rows where a sequence has no more on average (single tokens), or where all blocks together are few, so that their keys are divided over many workgroups:
-// pieces of 32 rows are joined sooner than pieces of 256.  Else a block of 256 rows uses a tile of K and V eight times as often.  us, 32 | 256, sequences x new tokens on
-// tokens before: d = 128, 32 / 8 heads 1 x 32 on 16000 (32 blocks of 32 rows) 53 | 65, 1 x 64 on 2000 (64) 29 | 39, on 16000 83 | 76, 1 x 128 on 2000 (128) 38 | 44, on 16000 145 | 76, 8 x 16 on
-// 2000 (128) 37 | 29, 32 x 4 on 2000 (a block a sequence) 53 | 53; d = 64, 16 / 4 heads 1 x 128 on 16000 (64) 48 | 68, 8 x 32 on 2000 (128) 23 | 30, on 16000 79 | 55, 8 x 128 on 2000 52 | 35.
+// pieces of 32 rows are joined sooner than larger ones.  Else larger blocks use a tile of K and V four or eight times as often.  us, 32 rows | larger, with the join, sequences x new
+// tokens on tokens before.  d = 128, 32 / 8 heads: 1 x 1 on 4000 17 | 22, on 30000 33 | 39, 256 x 1 on 100 40 | 56, 64 x 1 on 4000 195 | 188, 120 x 1 and 1 x 256 on 2000 211 | 245;
+// 1 x 16 on 16000 (16 blocks of 32 rows) 35 | 33, 1 x 32 (32) 48 | 36, 1 x 128 (128) 138 | 59, 8 x 16 on 2000 (120) 36 | 24.  d = 64, 16 / 4 heads: 1 x 1 on 4000 11 | 17, on 30000 20 | 35;
+// 1 x 32 on 16000 (16) 25 | 31, 1 x 64 on 2000 (32) 18 | 18, on 16000 28 | 33, 1 x 128 (64) 39 | 38, 8 x 16 on 2000 (92) 21 | 19, 32 x 32 on 2000 39 | 27.
 inline PagedShape paged_shape(int64_t rows, int B, int Hk, int d) {
-  if (rows <= (int64_t)32 * B || Hk * ((rows + 31) / 32 + B - 1) <= 64) return {32, paged_one_slots(d)};
-  return {256, paged_rows_slots(d)};
+  if (rows <= (int64_t)32 * B || Hk * ((rows + 31) / 32 + B - 1) < 32) return {32, paged_one_slots(d)};
+  return {paged_block_rows(d), paged_rows_slots(d)};
 }
 // The number of slots and what to join at each of them (Join in attn_paged_line.h), then two pieces a slot: 32-bit rows of O and three statistics.  Room for either
 // kernel, so that a workspace serves every call at its head dimension.
@@ -92,7 +96,7 @@ inline size_t paged_part_bytes(const PagedShape& s, int d) {
   return (size_t)(s.slots + 1) * kJoinBytes + (size_t)2 * s.slots * s.rows * ((d <= 32 ? 32 : d) + 4) * sizeof(float);
 }
 inline size_t paged_workspace_bytes(int d) {
-  const size_t one = paged_part_bytes({32, paged_one_slots(d)}, d), rows = paged_part_bytes({256, paged_rows_slots(d)}, d);
+  const size_t one = paged_part_bytes({32, paged_one_slots(d)}, d), rows = paged_part_bytes({paged_block_rows(d), paged_rows_slots(d)}, d);
   return one > rows ? one : rows;
 }
 

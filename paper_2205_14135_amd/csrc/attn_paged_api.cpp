@@ -54,7 +54,8 @@ bool page_size_ok(int n) { return n >= 16 && n <= 4096 && (n & (n - 1)) == 0; }
 int check_caches(int pages, int Hk, int page_size, int d, int64_t sp, int64_t sh, int64_t sn) {
   if (pages <= 0 || Hk <= 0 || Hk > (1 << 16)) return ATTN_ERR_SHAPE;
   if (!page_size_ok(page_size)) return ATTN_ERR_PAGES;
-  if (sn > ((int64_t)1 << 23)) return ATTN_ERR_SHAPE;   // a tile copy addresses its rows with 32-bit byte offsets
+  // a page, and the step from one page to the next, are less than 4 GiB (tile copies address rows by 32-bit byte offsets)
+  if (sn > ((int64_t)1 << 23) || sn * page_size >= (int64_t)1 << 31 || sp >= (int64_t)1 << 31) return ATTN_ERR_SHAPE;
   const Axis p = {sp, pages}, h = {sh, Hk}, n = {sn, page_size};
   return rows_ok({p, h, n}) && rows_apart(d, p, h, n) ? ATTN_OK : ATTN_ERR_SHAPE;
 }
@@ -80,6 +81,7 @@ int check_batch(const attn_paged_params* p, attn::PagedBatch* out) {
   b.pages = p->pages; b.page_log2 = log2_of(p->page_size); b.width = p->table_width;
   b.capacity = p->table_width << b.page_log2;
   b.sp = p->page_stride; b.sh = p->head_stride; b.sn = p->row_stride;
+  b.page_bytes = (uint32_t)(2 * p->page_stride); b.row_bytes = (uint32_t)(2 * p->row_stride); b.page_mask = (uint32_t)p->page_size - 1;
   return ATTN_OK;
 }
 int check_batch_pointers(const attn::PagedBatch& b) {

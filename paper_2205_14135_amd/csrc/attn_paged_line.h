@@ -69,6 +69,13 @@ __device__ __forceinline__ double lane_double(double v, int lane) {
   return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
 }
 
+// A double that all lanes share, in scalar registers: the arithmetic is the vector unit's, and the tile loops have no vector registers to keep it in.
+__device__ __forceinline__ double uniform(double v) { return lane_double(v, 0); }
+__device__ __forceinline__ void uniform(Sequence& s) {
+  s.a = uniform(s.a);
+  s.step = uniform(s.step);
+}
+
 // A point of the line: item (sequence b, K head h, block t), where on the line that starts, and the distance z from there.
 struct Point {
   int b, h, t;
@@ -168,7 +175,7 @@ __device__ __forceinline__ Join* join_list(const PagedCall& c) { return (Join*)(
 
 // The item behind `at`, whose stretch ends at x on the line: false if there is none.  s: its sequence, of at before.
 template <class DIV> __device__ __forceinline__ bool next_item(const PagedCall& c, double x, Point& at, Sequence& s) {
-  at.at = x;
+  at.at = uniform(x);
   at.z = 0.0;
   if (++at.t < s.blocks) return true;
   at.t = 0;
@@ -177,20 +184,11 @@ template <class DIV> __device__ __forceinline__ bool next_item(const PagedCall& 
   do {
     if (++at.b >= c.b.B) return false;
     s = load_sequence_uniform<DIV>(c, at.b);
+    uniform(s);
   } while (s.rows == 0);
   return true;
 }
 
-// The stretch of a slot: from `at` (s: its sequence) to x_end.  False: there is none.  `numbers`: of the first 64 sequences, loaded before the kernel does what else it can.
-template <class DIV> __device__ __forceinline__ bool stretch(const PagedCall& c, const Numbers& numbers, Line<DIV>& line, int& slot, Point& at, Sequence& s, double& x_end) {
-  line.init(c, numbers);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *join_slots(c) = line.total == 0.0 ? 0 : line.n;
-  slot = xcd_item(line.n, (line.n + kXcds - 1) / kXcds);   // neighbours on the line share an XCD's L2
-  if (slot < 0 || line.total == 0.0) return false;
-  at = line.locate(c, line.start(slot), s);
-  x_end = line.start(slot + 1);
-  return true;
-}
 // What there is to join at the start of a slot's stretch, left in the workspace.
 template <class DIV> __device__ __forceinline__ void leave_join(const PagedCall& c, const Line<DIV>& line, int slot, const Point& at, const Sequence& s) {
   if (slot == 0) return;
@@ -208,19 +206,47 @@ template <class DIV> __device__ __forceinline__ void leave_join(const PagedCall&
     join_list(c)[slot] = j;
   }
 }
-// Moves a cut at the start of a stretch.  False: there is nothing behind it.
-template <class DIV> __device__ __forceinline__ bool from_here(const PagedCall& c, const Line<DIV>& line, Point& at, Sequence& s) {
-  const double v = s.length(at.t);
-  if (at.z <= line.slack) at.z = 0.0;
-  else if (v - at.z <= line.slack) return next_item<DIV>(c, at.at + v, at, s);
-  return true;
-}
-// Where a stretch that ends at x_end on the line ends in the item at `at`, v long: 0 in front of it, v at its end or behind.
-template <class DIV> __device__ __forceinline__ double up_to_here(const Line<DIV>& line, int slot, const Point& at, double v, double x_end) {
-  const double z1 = x_end - at.at;
-  if (slot + 1 < line.n && z1 <= line.slack) return 0.0;
-  return v - z1 <= line.slack ? v : z1;
-}
+// What a workgroup does: the items of its stretch, one after the other.
+template <class DIV> struct Work {
+  Line<DIV> line;
+  Point at;          // the item, from distance at.z from its start ...
+  Sequence s;        // ... of this sequence
+  int slot;
+  double x_end;      // the stretch's end
+
+  // numbers: of the first 64 sequences, loaded before the kernel does what else it can.  False: there is nothing to do.  Leaves in the workspace how many slots there are, and
+  // what there is to join.
+  __device__ __forceinline__ bool begin(const PagedCall& c, const Numbers& numbers) {
+    line.init(c, numbers);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *join_slots(c) = line.total == 0.0 ? 0 : line.n;
+    if (line.total == 0.0) return false;
+    slot = xcd_item(line.n, (line.n + kXcds - 1) / kXcds);   // neighbours on the line share an XCD's L2
+    if (slot < 0) return false;
+    at = line.locate(c, line.start(slot), s);
+    x_end = line.start(slot + 1);
+    leave_join<DIV>(c, line, slot, at, s);
+    // a cut near an item's end is made there
+    const double v = s.length(at.t);
+    if (at.z <= line.slack) at.z = 0.0;
+    else if (v - at.z <= line.slack && !next_item<DIV>(c, at.at + v, at, s)) return false;
+    x_end = uniform(x_end);
+    line.slack = uniform(line.slack);
+    at.at = uniform(at.at);
+    at.z = uniform(at.z);
+    uniform(s);
+    return true;
+  }
+  // Where the stretch ends in the item, v long: v at its end or behind, 0 in front of it.
+  __device__ __forceinline__ double up_to(double v) const {
+    const double z1 = x_end - at.at;
+    if (slot + 1 < line.n && z1 <= line.slack) return 0.0;
+    return uniform(v - z1 <= line.slack ? v : z1);
+  }
+  __device__ __forceinline__ bool next(const PagedCall& c, double v) {
+    const double x = at.at + v;
+    return x < x_end && next_item<DIV>(c, x, at, s);
+  }
+};
 
 // row / G
 __device__ __forceinline__ int token_of(const PagedCall& c, int row) { return (int)(((uint64_t)(uint32_t)row * c.g_factor) >> c.g_shift); }

@@ -196,7 +196,6 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
   const Numbers numbers = Round::numbers(c, 0);   // (on their way while the lane's constants are made)
   const int lane = threadIdx.x, r = lane & 31, g = lane >> 5;
   const float cs = c.scale_log2;
-  const int page_mask = (1 << c.b.page_log2) - 1;
   TrOffsets<D> tro;
   tro.init();
   uint32_t goff[COPIES];   // byte offset of this lane's chunk of a copy from the copy's first row
@@ -215,17 +214,14 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
   asm volatile("" ::"v"(tro.off[0][0]), "v"(goff[0]), "v"(goff[COPIES - 1]));
 #endif
 
-  Line<Div> line;
-  int slot;
-  Point at;
-  Sequence s;
-  double x_end;
-  if (!stretch<Div>(c, numbers, line, slot, at, s, x_end)) return;
-  leave_join<Div>(c, line, slot, at, s);
-  if (!from_here<Div>(c, line, at, s)) return;
+  Work<Div> work;
+  if (!work.begin(c, numbers)) return;
+  const Point& at = work.at;
+  const Sequence& s = work.s;
+
   while (true) {
-    const double length = s.length(at.t);
-    const double z1 = up_to_here(line, slot, at, length, x_end);
+    const double length = uniform(s.length(at.t));
+    const double z1 = work.up_to(length);
     if (z1 == 0.0) break;
     const int tiles = tiles_of<BR>(c, s, at.t, KEYS);
     const int j0 = cut_at(at.z, length, tiles), j1 = cut_at(z1, length, tiles);
@@ -255,13 +251,13 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
       if (all) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-          const int64_t off = (int64_t)ids[i] * c.b.sp + (int64_t)((j * KEYS + 16 * i) & page_mask) * c.b.sn;
+          const uint64_t off = (uint64_t)(uint32_t)ids[i] * c.b.page_bytes + (uint32_t)((j * KEYS + 16 * i) & c.b.page_mask) * c.b.row_bytes;
 #pragma unroll
           for (int p = i * PER_PAGE; p < (i + 1) * PER_PAGE; ++p) {
-            const int64_t row = (p - i * PER_PAGE) * RPC * c.b.sn;
+            const uint64_t at_row = off + (p - i * PER_PAGE) * RPC * c.b.row_bytes;
             if (D != 32 || !((beyond >> p) & 1u)) {
-              async_copy_b128(Kg + off + row, goff[p], k_lds + p * 1024);
-              async_copy_b128(Vg + off + row, goff[p], v_lds + p * 1024);
+              async_copy_b128((const char*)Kg + at_row, goff[p], k_lds + p * 1024);
+              async_copy_b128((const char*)Vg + at_row, goff[p], v_lds + p * 1024);
             }
           }
         }
@@ -270,10 +266,10 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
 #pragma unroll
         for (int p = 0; p < COPIES; ++p) {
           const int id = ids[p / PER_PAGE], row = j * KEYS + p * RPC;
-          const int64_t off = (int64_t)id * c.b.sp + (int64_t)(row & page_mask) * c.b.sn;
+          const uint64_t off = (uint64_t)(uint32_t)id * c.b.page_bytes + (uint32_t)(row & c.b.page_mask) * c.b.row_bytes;
           const bool there = (uint32_t)id < (uint32_t)c.b.pages && row + lane_row < L;
-          const void* const kp = there ? (const void*)((const char*)(Kg + off) + goff[p]) : (const void*)zero_line;
-          const void* const vp = there ? (const void*)((const char*)(Vg + off) + goff[p]) : (const void*)zero_line;
+          const void* const kp = there ? (const void*)((const char*)Kg + off + goff[p]) : (const void*)zero_line;
+          const void* const vp = there ? (const void*)((const char*)Vg + off + goff[p]) : (const void*)zero_line;
           if (D != 32 || !((beyond >> p) & 1u)) {
             async_copy_b128(kp, k_lds + p * 1024);
             async_copy_b128(vp, v_lds + p * 1024);
@@ -344,9 +340,8 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
 
     const float l_tot = l_run + xchg32(l_run), lr_sum = lr_run + xchg32(lr_run);
     if (at.z == 0.0 && z1 == length) write_rows<T, D>(c, s, at.h, at.t * BR, o, m_run, l_tot, lr_sum, &Ks[0][0]);
-    else write_piece<D>(c, s, at.t, piece_index(slot, at.z == 0.0), o, m_run, l_tot, lr_sum);
-    const double x = at.at + length;
-    if (x >= x_end || !next_item<Div>(c, x, at, s)) break;
+    else write_piece<D>(c, s, at.t, piece_index(work.slot, at.z == 0.0), o, m_run, l_tot, lr_sum);
+    if (!work.next(c, length)) break;
   }
 }
 

@@ -108,6 +108,18 @@ def test_paged_fwd_refuses(lib, kw, status):
     assert (lib.attn_paged_workspace_bytes(ctypes.byref(p)) == 0) != pointers
 
 
+@pytest.mark.parametrize("kw,ok", [
+    (dict(page_stride=(1 << 31) - 8), True), (dict(page_stride=1 << 31), False),                                     # bytes from page to page: 32 bits
+    (dict(page_size=4096, row_stride=(1 << 19) - 8, head_stride=64, page_stride=(1 << 31) - 8), True),
+    (dict(page_size=4096, row_stride=1 << 19, head_stride=64, page_stride=(1 << 31) - 8), False),                    # and inside a page
+    (dict(B=1 << 20, T=1 << 20), True), (dict(B=(1 << 20) + 1, T=(1 << 20) + 1), False)])
+def test_paged_limits(lib, kw, ok):
+    p = _paged(**kw)
+    assert (lib.attn_paged_workspace_bytes(ctypes.byref(p)) != 0) == ok
+    if not ok:
+        assert lib.attn_paged_fwd(ctypes.byref(p), OK_PTR, OK_PTR, OK_PTR, OK_PTR, OK_PTR, OK_PTR, 1 << 30) == -2
+
+
 def test_paged_fwd_pointers_and_workspace(lib):
     p = _paged()
     need = lib.attn_paged_workspace_bytes(ctypes.byref(p))
