@@ -70,13 +70,18 @@ def rotary_embedding(q: torch.Tensor, k: torch.Tensor, rotary: Rotary, positions
     """(q', k'): q and k turned by their tokens' positions, differentiable with respect to both (any number of times).
 
     q, k: [B,H,N,d] fp16 or bf16 CUDA tensors, d contiguous, d in {16, 32, 64, 128}; their numbers of heads and strides may differ.  positions:
-    int32 [N] or [B,N] (default 0 .. N - 1).  One launch forward, one backward.
+    int32 [N] or [B,N] (default 0 .. N - 1).  One launch forward, one backward.  In a captured graph that holds the backward pass too, no eager graph may lead to the same
+    leaves any more (drop its outputs first): a forward pass that meets one of the default stream is refused.
     """
+    return _turned(q, k, None, rotary, positions)
+
+
+def _turned(q, k, v, rotary, positions):
     if binding._lib is None:
         binding.load()
     if _node_in_python():
         return _RotaryEmbedding.apply(q, k, rotary.frequencies, rotary.interleaved, rotary.magnitude, positions, False)
-    return binding._marshal.rotary_embedding(q, k, rotary.frequencies, rotary.interleaved, rotary.magnitude, positions)
+    return binding._marshal.rotary_embedding(q, k, rotary.frequencies, rotary.interleaved, rotary.magnitude, positions, v)
 
 
 def flash_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, softmax_scale: Optional[float] = None,
@@ -102,7 +107,7 @@ def flash_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, softma
     if binding._lib is None:
         binding.load()
     if rotary is not None:
-        q, k = rotary_embedding(q, k, rotary, positions)
+        q, k = _turned(q, k, v, rotary, positions)
     elif positions is not None:
         raise ValueError("positions are of no use without rotary")
     if _node_in_python():

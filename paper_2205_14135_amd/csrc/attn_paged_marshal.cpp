@@ -4,9 +4,11 @@
 #include "attn_marshal.h"
 
 #include <c10/core/DeviceGuard.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <torch/csrc/autograd/function.h>
 #include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/saved_variable.h>
+#include <torch/csrc/autograd/variable.h>
 
 namespace {
 
@@ -206,13 +208,29 @@ variable_list rotary_embedding(const at::Tensor& q, const at::Tensor& k, const R
   return {qo, ko};
 }
 
-// rotary_embedding(Q, K, frequencies, interleaved, magnitude, positions) -> (Q', K'), differentiable
+// The node that sums a leaf's gradient lives as long as any graph that leads to the leaf, and keeps the stream it was made on.  A captured backward pass that meets one of the
+// default stream makes that stream wait for the capture, which ends the process; so the forward pass refuses.
+void refuse_eager_graphs(std::initializer_list<const at::Tensor*> leaves) {
+  if (c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None) return;
+  for (const at::Tensor* t : leaves) {
+    if (!t->defined() || !t->is_leaf() || !t->requires_grad()) continue;
+    const std::shared_ptr<torch::autograd::Node> sum = torch::autograd::impl::try_get_grad_accumulator(*t);
+    if (sum != nullptr && sum->stream().has_value() && sum->stream()->id() == 0)
+      raise(PyExc_RuntimeError, "captured while a graph made on the default stream still leads to the same leaf: drop that graph (its outputs) first, or make it on another stream");
+  }
+}
+
+// rotary_embedding(Q, K, frequencies, interleaved, magnitude, positions, V) -> (Q', K'), differentiable.  V: a leaf of the same pass, or None.
 PyObject* py_rotary_embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    expect_args(n, 6);
-    const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]);
+    expect_args(n, 7);
+    const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), v = maybe(a[6]);
     const Rotation r = {tensor(a[2]), maybe(a[5]), truth(a[3]), false, number(a[4])};
     check_rotation(q, k, r);
+    if (at::GradMode::is_enabled()) {
+      const c10::DeviceGuard guard(q.device());
+      refuse_eager_graphs({&q, &k, &v});
+    }
     variable_list out;
     {
       PyThreadState* const s = PyEval_SaveThread();

@@ -180,3 +180,27 @@ def test_graph_of_forward_and_backward():
         want = step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(replayed, want))
+
+
+@pytest.mark.parametrize("call", ["rotary", "attention", "attention_v"])
+def test_capture_beside_an_eager_graph_is_refused(call):
+    """The forward pass under capture is refused while an eager graph of the default stream leads to a leaf; without that graph it is not."""
+    f, _ = rotary_frequencies(64)
+    rotary = Rotary(f.cuda())
+    q, k, v = (_tensor(1, 2, 40, 64, "bf16", 60 + i).requires_grad_(call != "attention_v" or i == 2) for i in range(3))
+    run = (lambda: rotary_embedding(q, k, rotary)) if call == "rotary" else (lambda: flash_attention(q, k, v, rotary=rotary))
+    held = run()
+    here = torch.zeros(1, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        here.add_(1)
+        with pytest.raises(RuntimeError, match="still leads to the same leaf"):
+            run()
+    with torch.no_grad(), torch.cuda.graph(torch.cuda.CUDAGraph()):
+        run()
+    del held
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        run()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert here.item() == 1.0
