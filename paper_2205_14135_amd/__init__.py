@@ -1,4 +1,4 @@
-"""MI355X-native IO-aware exact attention (forward, backward, causal, dropout, block-sparse).
+"""MI355X-native IO-aware exact attention (forward, backward, causal, dropout, block-sparse), rotary positions, and attention over a paged key/value cache.
 
 The compute path is the HIP library under csrc/ reached through the C ABI
 declared in include/attn.h; `binding` marshals arguments only.  `inputs`

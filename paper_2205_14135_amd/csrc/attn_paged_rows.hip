@@ -5,7 +5,7 @@
 // does its softmax; K and V tiles of 64 keys in rings of three, group A copies K and group B V.
 //   d <= 64: four wavefronts of 32 rows, three workgroups to a compute unit (attn_fwd.hip).
 // us, blocks of 128 rows | 256, the main kernel, causal, 16 heads: d = 32, 4 x 4096 tokens 152 | 204; d = 64, a chunk of 1000 tokens among 32 single ones, contexts up to 4000, 22.5 | 28.5;
-// d = 128, 2 x 8192 slower by a tenth in blocks of 128.
+// d = 128, 2 x 8192 tokens 620 | 560, not causal 1036 | 967.
 //   Pages: a wavefront copies 16 rows of a tile, which lie in one page.  Its page number is a lane of a register that holds those of sixteen tiles, loaded sixteen tiles
 // ahead: the address of a copy is scalar work alone.  (One load a tile, used in the next, makes the compiler wait for the copies issued since: its count
 // of loads in flight does not know them.)
