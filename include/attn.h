@@ -356,7 +356,7 @@ typedef struct {
 
 /*
  * Writes the new tokens' K and V rows into the pages, token i of the m new ones of sequence b at position lengths[b] - m + i (a position that is negative, or behind
- * the table's last page, is not written).  With rotary != NULL K is turned by its position, and so is Q, if one is given, into Qout (in place where
+ * the table's last page, is not written).  Where the table gives two tokens of a call the same row, one of them is what stands there.  With rotary != NULL K is turned by its position, and so is Q, if one is given, into Qout (in place where
  * Qout == Q with the same strides).  rotary == NULL: K is copied; then Q must be NULL.
  */
 int attn_paged_append(const attn_paged_params* p, const attn_rotary_spec* rotary, const void* K, const void* V, void* k_cache, void* v_cache, const void* Q,

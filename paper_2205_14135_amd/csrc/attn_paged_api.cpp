@@ -55,6 +55,7 @@ int check_caches(int pages, int Hk, int page_size, int d, int64_t sp, int64_t sh
   if (pages <= 0 || Hk <= 0 || Hk > (1 << 16)) return ATTN_ERR_SHAPE;
   if (!page_size_ok(page_size)) return ATTN_ERR_PAGES;
   // a page, and the step from one page to the next, are less than 4 GiB (tile copies address rows by 32-bit byte offsets)
+  if ((int64_t)Hk * page_size * d > (int64_t)1 << 33) return ATTN_ERR_SHAPE;   // (a copy counts a page's 16-byte pieces in 32 bits)
   if (sn > ((int64_t)1 << 23) || sn * page_size >= (int64_t)1 << 31 || sp >= (int64_t)1 << 31) return ATTN_ERR_SHAPE;
   const Axis p = {sp, pages}, h = {sh, Hk}, n = {sn, page_size};
   return rows_ok({p, h, n}) && rows_apart(d, p, h, n) ? ATTN_OK : ATTN_ERR_SHAPE;
@@ -107,9 +108,9 @@ int check_paged(const attn_paged_params* p, attn::PagedCall* out, attn::PagedSha
   c.scale_log2 = (float)((double)p->softmax_scale * 1.4426950408889634);
   *shape = attn::paged_shape((int64_t)p->T * c.G, p->B, p->Hk, p->d);
   c.slots = shape->slots;
-  // the line that the work is laid out on (attn_paged_line.h), at its longest, times the slots, in 62 bits
+  // the line that the work is laid out on (attn_paged_line.h), at its longest (256: what an item costs beside its keys, at most)
   const double rows = (double)p->T * c.G, blocks = rows / shape->rows + p->B;
-  if (p->Hk * (blocks * c.G * ((double)c.b.capacity + 64) + rows * (blocks + 1)) > 0x1p50) return ATTN_ERR_SHAPE;
+  if (p->Hk * (blocks * c.G * ((double)c.b.capacity + 256) + rows * (blocks + 1)) > 0x1p50) return ATTN_ERR_SHAPE;
   return ATTN_OK;
 }
 

@@ -223,11 +223,12 @@ __global__ __launch_bounds__(NT) void append_kernel(const AppendCall c, const in
   }
 }
 
-// Heads a thread walks over: as many as leave 8 wavefronts a SIMD's worth of threads (its angles are then computed once for all of them), at most 8.
+// Heads a thread walks over: as many as leave 8 wavefronts a SIMD's worth of threads (its angles are then computed once for all of them), at most 8; and at least so many
+// that a grid's second axis holds the rest.
 int heads_per_thread(int64_t token_units, int heads) {
   const int64_t enough = (int64_t)kComputeUnits * 8 * 64;
   int per = 8;
-  while (per > 1 && token_units * ((heads + per - 1) / per) < enough) per /= 2;
+  while (per > 1 && token_units * ((heads + per - 1) / per) < enough && (heads + per / 2 - 1) / (per / 2) < 65536) per /= 2;
   return per;
 }
 int log2_units(int d) { return d == 128 ? 3 : (d == 64 ? 2 : (d == 32 ? 1 : 0)); }

@@ -246,3 +246,19 @@ def test_sequences_forked_ended_and_compacted():
     step([e, b, c], [1, 1, 1])
     g = fork(e)
     step([g, e, b, c], [1, 1, 30, 1])
+
+
+def test_append_of_very_many_heads():
+    """Position 0 turns nothing: K, V and Q arrive as they are."""
+    H = 65536
+    f, _ = rotary_frequencies(16)
+    gen = torch.Generator().manual_seed(90)
+    q, k, v = (torch.randn(1, H, 16, generator=gen).to(torch.bfloat16).cuda() for _ in range(3))
+    kc, vc = (torch.full((2, H, 16, 16), 3.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table, lengths = torch.tensor([[1]], dtype=torch.int32).cuda(), torch.tensor([1], dtype=torch.int32).cuda()
+    out = binding.attn_paged_append(k, v, kc, vc, table, lengths, Q=q, rotary=Rotary(f.cuda()))
+    assert torch.equal(out, q)
+    for cache, x in ((kc, k), (vc, v)):
+        assert torch.equal(cache[1, :, 0], x[0])
+        cache[1, :, 0] = 3.0
+        assert bool((cache == 3.0).all())

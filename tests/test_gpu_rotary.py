@@ -204,3 +204,13 @@ def test_capture_beside_an_eager_graph_is_refused(call):
     graph.replay()
     torch.cuda.synchronize()
     assert here.item() == 1.0
+
+
+def test_very_many_heads():
+    f, _ = rotary_frequencies(16)
+    rotary = Rotary(f.cuda())
+    q, k = _tensor(1, 65536, 1, 16, "bf16", 70), _tensor(1, 65535, 1, 16, "bf16", 71)
+    pos = torch.tensor([5], dtype=torch.int32)
+    for x, y in zip((q, k), binding.attn_rotary(q, k, rotary, positions=pos.cuda())):
+        want, bound = _want(x, pos, f, False, 1.0)
+        ph.assert_within(y, want, bound, "y")

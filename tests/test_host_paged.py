@@ -112,6 +112,8 @@ def test_paged_fwd_refuses(lib, kw, status):
     (dict(page_stride=(1 << 31) - 8), True), (dict(page_stride=1 << 31), False),                                     # bytes from page to page: 32 bits
     (dict(page_size=4096, row_stride=(1 << 19) - 8, head_stride=64, page_stride=(1 << 31) - 8), True),
     (dict(page_size=4096, row_stride=1 << 19, head_stride=64, page_stride=(1 << 31) - 8), False),                    # and inside a page
+    (dict(Hq=1 << 16, Hk=1 << 16, d=128, page_size=1024, row_stride=128, page_stride=1 << 17, head_stride=10 << 17, q_stride_h=128, o_stride_h=128, q_stride_t=1 << 23, o_stride_t=1 << 23), True),
+    (dict(Hq=1 << 16, Hk=1 << 16, d=128, page_size=2048, row_stride=128, page_stride=1 << 18, head_stride=10 << 18, q_stride_h=128, o_stride_h=128, q_stride_t=1 << 23, o_stride_t=1 << 23), False),
     (dict(B=1 << 20, T=1 << 20), True), (dict(B=(1 << 20) + 1, T=(1 << 20) + 1), False)])
 def test_paged_limits(lib, kw, ok):
     p = _paged(**kw)
