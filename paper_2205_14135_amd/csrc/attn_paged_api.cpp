@@ -108,9 +108,9 @@ int check_paged(const attn_paged_params* p, attn::PagedCall* out, attn::PagedSha
   c.scale_log2 = (float)((double)p->softmax_scale * 1.4426950408889634);
   *shape = attn::paged_shape((int64_t)p->T * c.G, p->B, p->Hk, p->d);
   c.slots = shape->slots;
-  // the line that the work is laid out on (attn_paged_line.h), at its longest (256: what an item costs beside its keys, at most)
+  // the line that the work is laid out on (attn_paged_line.h), at its longest (320: what an item costs beside its keys, at most)
   const double rows = (double)p->T * c.G, blocks = rows / shape->rows + p->B;
-  if (p->Hk * (blocks * c.G * ((double)c.b.capacity + 256) + rows * (blocks + 1)) > 0x1p50) return ATTN_ERR_SHAPE;
+  if (p->Hk * (blocks * c.G * ((double)c.b.capacity + 320) + rows * (blocks + 1)) > 0x1p50) return ATTN_ERR_SHAPE;
   return ATTN_OK;
 }
 

@@ -12,11 +12,10 @@
 namespace attn {
 
 // How a kernel divides its line.  BR: rows of a block.  KEYS: of a tile.  ITEM: what an item costs beside its keys, in keys (Q, the wait for its first tile, its end); a piece costs
-// as much, and a join.  SPREAD: a stretch has at least the square root of SPREAD times the longest item's keys, so that joining the pieces takes no longer than making one:
+// as much, and a join.  SLACK: keys that a cut is moved by to an end of its item.  SPREAD: a stretch has at least the square root of SPREAD times the longest item's keys, so that joining the pieces takes no longer than making one:
 // with k keys in each of n / k pieces the kernel takes c k for a piece, the join C n / k, and the sum is least at k^2 = n C / c.
-template <int BR_, int KEYS_, int ITEM_, int SPREAD_> struct Division {
-  static constexpr int BR = BR_, KEYS = KEYS_, ITEM = ITEM_, SPREAD = SPREAD_;
-  static constexpr int SLACK = (ITEM + KEYS) / 2;   // keys that a cut is moved by to an end of its item: an item of one tile is never cut
+template <int BR_, int KEYS_, int ITEM_, int SLACK_, int SPREAD_> struct Division {
+  static constexpr int BR = BR_, KEYS = KEYS_, ITEM = ITEM_, SLACK = SLACK_, SPREAD = SPREAD_;
 };
 // A sequence of the batch, every number taken from device memory forced into its range.
 struct Sequence {

@@ -16,8 +16,10 @@
 namespace attn {
 namespace {
 
-typedef Division<256, 64, 256, 18> PairDiv;    // two groups of four wavefronts
-typedef Division<128, 64, 128, 18> BlockDiv;   // four wavefronts
+// us, ITEM and SLACK of 256 and 160 | 320 and 320, 128 and 96 | 256 and 256, 16 heads: d = 128, 8 x 256 tokens 25 | 18, 8 x 1024 67 | 67; d = 64, 8 x 256 22 | 14, 32 x 64 on 100 20 | 13, 4 x 4096
+// 195 | 195.  Over 76 batches, 32 of them ragged, the same within 1 per cent at d = 128, 6 to 8 less at d = 64; 25 per cent more or less of either changes nothing.
+typedef Division<256, 64, 320, 320, 18> PairDiv;    // two groups of four wavefronts
+typedef Division<128, 64, 256, 256, 18> BlockDiv;   // four wavefronts
 constexpr int BC = 64;
 
 // The copies of a tile that a wavefront makes: 16 rows, which lie in one page.  Page numbers come sixteen tiles at a time, those of their 16-row groups one a lane.
@@ -210,11 +212,6 @@ __global__ __launch_bounds__(512) void paged_pair_kernel(const PagedCall c) {
 
     if (J > 0) {
       const T* const Tg = (const T*)(group_b ? c.V : c.K) + (int64_t)at.h * c.b.sh;   // what this group copies
-      if (D == 32 && c.d < D) {   // head dimension 16: the copies leave columns >= 16 untouched
-        zero_tiles(&Ks[0][0], 3 * BC * D);
-        zero_tiles(&Vs[0][0], 3 * BC * D);
-        __syncthreads();
-      }
       Copies dma;
       dma.init(c, at.b, L, wave & 3, j0, lane);
       const uint32_t ring0 = __builtin_amdgcn_readfirstlane(lds_addr(group_b ? &Vs[0][0] : &Ks[0][0]) + dma.part * Copies::COPIES * 1024);
