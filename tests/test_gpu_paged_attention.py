@@ -313,3 +313,69 @@ def test_two_host_threads():
     assert not errors
     for g, w in zip(got, want):
         assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])
+
+
+# ---- the larger blocks (many rows a sequence): more than sixteen tiles of page numbers, cuts, bad numbers, rows that are no numbers
+
+BLOCKS = pytest.mark.parametrize("d,page,Hq,Hk", [(16, 16, 4, 2), (32, 32, 4, 4), (64, 16, 8, 2), (64, 256, 3, 3), (128, 16, 8, 2), (128, 64, 4, 4)])
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@BLOCKS
+def test_chunks_on_long_contexts(causal, d, page, Hq, Hk):
+    check(ph.Batch([2500, 1023, 0, 1500, 4000], [300, 129, 511, 1, 70], Hq, Hk, d, "bf16", page, pad=7, seed=100 + d), causal)
+
+
+@BLOCKS
+def test_chunks_and_numbers_that_are_no_page(d, page, Hq, Hk):
+    batch = ph.Batch([1300, 400], [260, 200], Hq, Hk, d, "fp16", page, seed=110 + d)
+    last = (1560 - 1) // page
+    for b, t, number in ((0, 0, -1), (0, 2, batch.pages), (0, last, 2 ** 31 - 1), (1, 1, -2 ** 31), (1, 599 // page, batch.pages + 1)):
+        batch.table[b, t] = number
+    check(batch)
+
+
+@BLOCKS
+def test_rows_of_chunks_that_see_nothing(d, page, Hq, Hk):
+    """More new tokens than the sequence is long: the first of them stand in front of it."""
+    check(ph.Batch([-250, -300, 200], [400, 300, 40], Hq, Hk, d, "bf16", page, seed=120 + d))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_of_a_chunk_that_are_no_numbers_stay_alone(d):
+    batch = ph.Batch([300, 80], [200, 150], 4, 2, d, "bf16", 16, seed=130)
+    want, want_l, bound, bound_l = ph.attention(batch, True)
+    batch.q[2, 1, 5] = math.nan
+    batch.q[205, 0, 0] = math.inf
+    q, kc, vc, table, lengths, starts = batch.gpu()
+    out, lse = binding.attn_paged_fwd(q, kc, vc, table, lengths, starts, softmax_scale=batch.tau)
+    assert torch.isnan(out[2, 1]).all() and torch.isnan(lse[1, 2])
+    bound[2, 1], bound[205, 0] = math.inf, math.inf
+    bound_l[1, 2], bound_l[0, 205] = math.inf, math.inf
+    ph.assert_within(torch.nan_to_num(out), want, bound, "O")
+    ph.assert_within(torch.nan_to_num(lse), want_l, bound_l, "LSE")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_lengths_and_starts_of_chunks_out_of_range_stay_inside(d):
+    batch = ph.Batch([47, 20], [300, 200], 4, 2, d, "bf16", 16, pad=5, seed=140)
+    q, kc, vc, table, lengths, starts = batch.gpu()
+    kc, vc = torch.nan_to_num(kc), torch.nan_to_num(vc)
+    for n, s in (([2 ** 31 - 1, -2 ** 31], [0, 300, 500]), ([347, 220], [-9, 2 ** 31 - 1, 3]), ([347, 220], [400, 3, 1]), ([0, -1], [2 ** 31 - 1] * 3), ([347, 220], [-2 ** 31, 505, 2 ** 31 - 1])):
+        out = torch.full_like(q, 7.0)
+        binding.attn_paged_fwd(q, kc, vc, table, torch.tensor(n, dtype=torch.int32).cuda(), torch.tensor(s, dtype=torch.int32).cuda(), softmax_scale=0.1, out=out)
+    torch.cuda.synchronize()
+    out, _ = binding.attn_paged_fwd(q, kc, vc, table, lengths, starts, softmax_scale=batch.tau)
+    want, _, bound, _ = ph.attention(batch, True)
+    ph.assert_within(out[:batch.tokens], want, bound, "O")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("scale", [8.0, 30.0])
+def test_peaked_rows_of_chunks(scale, d):
+    check(ph.Batch([900, 64, 1500], [133, 290, 200], 4, 2, d, "bf16", 16, seed=150), tau=scale / math.sqrt(d))
+
+
+@pytest.mark.parametrize("d,interleaved", [(64, False), (128, True)])
+def test_chunks_in_views_of_a_projection_and_another_order_of_axes(d, interleaved):
+    check(ph.Batch([500, 0, 1200], [170, 330, 1], 6, 2, d, "fp16", 32, pad=4, seed=160, token_major=interleaved, fused=True))
