@@ -379,3 +379,23 @@ def test_peaked_rows_of_chunks(scale, d):
 @pytest.mark.parametrize("d,interleaved", [(64, False), (128, True)])
 def test_chunks_in_views_of_a_projection_and_another_order_of_axes(d, interleaved):
     check(ph.Batch([500, 0, 1200], [170, 330, 1], 6, 2, d, "fp16", 32, pad=4, seed=160, token_major=interleaved, fused=True))
+
+
+@pytest.mark.parametrize("Hk,d", [(16, 64), (8, 128)])
+def test_chunks_in_caches_beyond_32_bit_offsets(Hk, d):
+    """More than 4 GiB of K: pages at both ends of the cache."""
+    page = 64
+    pages = (5 << 30) // (2 * page * Hk * d)
+    batch = ph.Batch([700, 90], [150, 300], Hk, Hk, d, "bf16", page, seed=170, extra_pages=0)
+    q, small_k, small_v, table, lengths, starts = batch.gpu()
+    place = torch.tensor([i if i % 2 else pages - 1 - i for i in range(batch.pages)], device="cuda")
+    caches = []
+    for small in (small_k, small_v):
+        big = torch.empty(pages, Hk, page, d, dtype=small.dtype, device="cuda")
+        big[place] = small
+        caches.append(big)
+    moved = torch.where(table >= 0, place[table.clamp(min=0).long()].to(torch.int32), table)
+    out, lse = binding.attn_paged_fwd(q, *caches, moved, lengths, starts, softmax_scale=batch.tau)
+    want, want_l, bound, bound_l = ph.attention(batch, True)
+    ph.assert_within(out, want, bound, "O")
+    ph.assert_within(lse, want_l, bound_l, "LSE")

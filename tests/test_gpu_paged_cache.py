@@ -262,3 +262,23 @@ def test_append_of_very_many_heads():
         assert torch.equal(cache[1, :, 0], x[0])
         cache[1, :, 0] = 3.0
         assert bool((cache == 3.0).all())
+
+
+def test_append_and_copy_beyond_32_bit_offsets():
+    """More than 4 GiB of K: the last page is written, and copied to the front and back; its neighbours stay."""
+    page, Hk, d = 64, 8, 128
+    pages = (5 << 30) // (2 * page * Hk * d)
+    kc, vc = (torch.empty(pages, Hk, page, d, dtype=torch.float16, device="cuda") for _ in range(2))
+    for c in (kc, vc):
+        c[:4] = 3.0
+        c[-4:] = 3.0
+    gen = torch.Generator().manual_seed(91)
+    k, v = (torch.randn(10, Hk, d, generator=gen).half().cuda() for _ in range(2))
+    table, lengths, starts = (torch.tensor(x, dtype=torch.int32).cuda() for x in ([[pages - 1]], [60], [0, 10]))
+    binding.attn_paged_append(k, v, kc, vc, table, lengths, starts)
+    binding.attn_paged_copy(kc, vc, [(pages - 1, 1), (0, pages - 3)])
+    for c, x in ((kc, k), (vc, v)):
+        want = torch.full((Hk, page, d), 3.0, dtype=torch.float16, device="cuda")
+        want[:, 50:60] = x.transpose(0, 1)
+        assert torch.equal(c[-1], want) and torch.equal(c[1], want)
+        assert all(bool((c[i] == 3.0).all()) for i in (0, 2, 3, -2, -3, -4))
