@@ -23,7 +23,7 @@ constexpr int NT = 256;
 //   kHalvesAny: the same columns, each partner read by itself
 enum Pairing { kHalves, kNeighbours, kHalvesAny };
 
-// cosine and sine, times the factor, of the angle at `position` of pair i (1, 0 behind the last)
+// cosine and sine, times the factor, of the angle at `position` of pair i (of no use behind the last)
 __device__ __forceinline__ void turn_of(const RotaryArgs& a, int position, int i, float& cs, float& sn) {
   cs = 1.f;
   sn = 0.f;
@@ -35,22 +35,26 @@ __device__ __forceinline__ void turn_of(const RotaryArgs& a, int position, int i
   sn = (a.inverse ? -s : s) * a.magnitude;
 }
 
-// The turn of one unit of one token, kept for all heads.
+// The turn of one unit of one token, kept for all heads.  What does not turn is copied, bit by bit: a product with cosine 1 and sine 0 would make NaN of an infinity in the
+// other column, and lose the sign of zeros.
 template <typename T, Pairing P> struct Turn {
   typedef typename Vec<T>::x8 T8;
   static constexpr int kAngles = P == kHalvesAny ? 16 : 8;
   int lo, hi;                     // first columns of the two pieces
   float cs[kAngles], sn[kAngles];
   int partner[P == kHalvesAny ? 16 : 1];   // kHalvesAny: the other column of a column's pair
+  int turning;                    // how many of the unit's pairs (kHalvesAny: columns) turn, its first ones; kHalves: all 8 or none
 
   __device__ __forceinline__ void columns(const RotaryArgs& a, int u) {
     if (P == kHalves) {
-      const int turning = a.r / 16;
-      lo = u < turning ? 8 * u : a.r + 16 * (u - turning);
-      hi = u < turning ? lo + a.r / 2 : lo + 8;
+      const int units = a.r / 16;   // that turn
+      lo = u < units ? 8 * u : a.r + 16 * (u - units);
+      hi = u < units ? lo + a.r / 2 : lo + 8;
+      turning = u < units ? 8 : 0;
     } else {
       lo = 16 * u;
       hi = lo + 8;
+      turning = P == kNeighbours ? a.r / 2 - 8 * u : a.r - 16 * u;
     }
   }
   __device__ __forceinline__ void angles(const RotaryArgs& a, int u, int position) {
@@ -77,6 +81,7 @@ template <typename T, Pairing P> struct Turn {
   __device__ __forceinline__ void turn_pieces(T8& a, T8& b, const T* x) const {
     T8 ya, yb;
     if constexpr (P == kHalves) {
+      if (turning == 0) return;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float fa = (float)a[e], fb = (float)b[e];
@@ -89,8 +94,8 @@ template <typename T, Pairing P> struct Turn {
         const T8& v = e < 4 ? a : b;
         const float fa = (float)v[(2 * e) & 7], fb = (float)v[(2 * e + 1) & 7];
         T8& w = e < 4 ? ya : yb;
-        w[(2 * e) & 7] = (T)(fa * cs[e] - fb * sn[e]);
-        w[(2 * e + 1) & 7] = (T)(fb * cs[e] + fa * sn[e]);
+        w[(2 * e) & 7] = e < turning ? (T)(fa * cs[e] - fb * sn[e]) : v[(2 * e) & 7];
+        w[(2 * e + 1) & 7] = e < turning ? (T)(fb * cs[e] + fa * sn[e]) : v[(2 * e + 1) & 7];
       }
     } else {
       float other[16];
@@ -98,8 +103,7 @@ template <typename T, Pairing P> struct Turn {
       for (int e = 0; e < 16; ++e) other[e] = (float)x[partner[e]];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const float own = (float)(e < 8 ? a[e & 7] : b[e & 7]);
-        const T v = (T)(own * cs[e] + other[e] * sn[e]);
+        const T own = e < 8 ? a[e & 7] : b[e & 7], v = e < turning ? (T)((float)own * cs[e] + other[e] * sn[e]) : own;
         if (e < 8) ya[e & 7] = v; else yb[e & 7] = v;
       }
     }
