@@ -49,6 +49,12 @@ struct PagedBatch {
   uint32_t page_bytes, row_bytes, page_mask;   // sp and sn in bytes; rows of a page - 1
 };
 
+// The rows first .. end - 1 of a sequence, out of its starts as they are in memory: forced into 0 .. T, for the append and for the attention alike.
+__device__ __forceinline__ void force_rows(const PagedBatch& b, int& first, int& end) {
+  first = min(max(first, 0), b.T);
+  end = min(max(end, first), b.T);
+}
+
 struct AppendCall {
   PagedBatch b;
   RotaryArgs rot;

@@ -50,7 +50,8 @@ struct Numbers {
   }
 };
 template <class DIV> __device__ __forceinline__ Sequence load_sequence(const PagedCall& c, const Numbers& n) {
-  const int first = min(max(n.first, 0), c.b.T), end = min(max(n.end, first), c.b.T);
+  int first = n.first, end = n.end;
+  force_rows(c.b, first, end);
   return sequence_of<DIV>(c, first, end - first, min(max(n.L, 0), c.b.capacity));
 }
 // the same for one that all lanes share, in scalar registers

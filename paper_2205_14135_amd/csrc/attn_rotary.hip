@@ -195,8 +195,10 @@ __global__ __launch_bounds__(NT) void append_kernel(const AppendCall c, const in
     b = sequence_of(p, token, 6 - units_log2);
     if (b >= p.B || token >= p.T) return;
     first = p.starts[b];
-    m = p.starts[b + 1] - first;
-    if (token < first) return;
+    int end = p.starts[b + 1];
+    force_rows(p, first, end);
+    if (token < first || token >= end) return;
+    m = end - first;
   } else if (b >= p.B) {
     return;   // (the host checks T >= B)
   }
