@@ -332,7 +332,8 @@ int attn_rotary(const attn_rotary_params* p, const attn_rotary_tensor* tensors, 
  *                  new tokens of sequence b, its last ones.  NULL: row b is the one new token of sequence b (then T >= B).
  *                  Rows of no sequence (behind the last, in a padded batch) are not read, and are left as they were in the outputs.
  * These three are read on the GPU only: a captured graph follows their contents.  Whatever they hold, nothing outside the tensors is
- * read or written: lengths are taken as at most table_width * page_size, starts as at most T, and a page
+ * read or written: starts are forced into 0 .. T; a sequence has as many keys as its length says, but no more than a row of its table holds, table_width * page_size
+ * (its new tokens keep the positions that its length gives them); and a page
  * number outside [0, pages) stands for a page of zeros that nothing is written to.  (Table entries behind a sequence's length are not used.)
  * What stands in the pages at positions < length must be finite; what stands behind is never used.
  */

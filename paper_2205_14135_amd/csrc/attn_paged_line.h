@@ -20,7 +20,8 @@ template <int BR_, int KEYS_, int ITEM_, int SLACK_, int SPREAD_> struct Divisio
 // A sequence of the batch, every number taken from device memory forced into its range.
 struct Sequence {
   int first;   // its first token's row of Q
-  int m, L;
+  int base;    // the position of its first new token: may be negative
+  int L;       // its keys: no more than a row of the table holds
   int rows, blocks;   // m * G, and in blocks of BR
   // The line's unit is 1 / G key; its points are whole numbers below 2^50 (the host checks that) in double: exact, and an instruction where a 64-bit integer takes four.
   // Block t is length(t) = a + step (t + 1) long (an upper bound of the keys its last row sees), the first t blocks are upto(t).
@@ -28,14 +29,14 @@ struct Sequence {
   __device__ __forceinline__ double length(int t) const { return a + step * (t + 1); }
   __device__ __forceinline__ double upto(int t) const { return t * a + step * (0.5 * t * (t + 1)); }
 };
-template <class DIV> __device__ __forceinline__ Sequence sequence_of(const PagedCall& c, int first, int m, int L) {
+template <class DIV> __device__ __forceinline__ Sequence sequence_of(const PagedCall& c, int first, int base, int L, int rows) {
   Sequence s;
   s.first = first;
-  s.m = m;
+  s.base = base;
   s.L = L;
-  s.rows = m * c.G;
+  s.rows = rows;
   s.blocks = (s.rows + DIV::BR - 1) / DIV::BR;
-  s.a = (double)c.G * ((c.causal ? max(L - m, 0) : L) + DIV::ITEM);
+  s.a = (double)c.G * ((c.causal ? max(min(base, L), 0) : L) + DIV::ITEM);
   s.step = c.causal ? DIV::BR : 0;
   return s;
 }
@@ -52,15 +53,19 @@ struct Numbers {
 template <class DIV> __device__ __forceinline__ Sequence load_sequence(const PagedCall& c, const Numbers& n) {
   int first = n.first, end = n.end;
   force_rows(c.b, first, end);
-  return sequence_of<DIV>(c, first, end - first, min(max(n.L, 0), c.b.capacity));
+  // (a length beyond what the table holds: the new tokens keep their positions, which are those that the append gives them, and see the keys that there are)
+  const int length = max(n.L, 0), m = end - first;
+  return sequence_of<DIV>(c, first, length - m, min(length, c.b.capacity), m * c.G);
 }
 // the same for one that all lanes share, in scalar registers
 template <class DIV> __device__ __forceinline__ Sequence load_sequence_uniform(const PagedCall& c, int b) {
   const Sequence s = load_sequence<DIV>(c, Numbers(c, b));
-  return sequence_of<DIV>(c, __builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.m), __builtin_amdgcn_readfirstlane(s.L));
+  return sequence_of<DIV>(c, __builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.base), __builtin_amdgcn_readfirstlane(s.L),
+                          __builtin_amdgcn_readfirstlane(s.rows));
 }
 template <class DIV> __device__ __forceinline__ Sequence lane_sequence(const PagedCall& c, const Sequence& s, int lane) {
-  return sequence_of<DIV>(c, __builtin_amdgcn_readlane(s.first, lane), __builtin_amdgcn_readlane(s.m, lane), __builtin_amdgcn_readlane(s.L, lane));
+  return sequence_of<DIV>(c, __builtin_amdgcn_readlane(s.first, lane), __builtin_amdgcn_readlane(s.base, lane), __builtin_amdgcn_readlane(s.L, lane),
+                          __builtin_amdgcn_readlane(s.rows, lane));
 }
 
 __device__ __forceinline__ double lane_double(double v, int lane) {
@@ -253,7 +258,7 @@ __device__ __forceinline__ int token_of(const PagedCall& c, int row) { return (i
 
 // What the 32 rows of an item from row0 on are: lane r has row `row0 + r` = token * G + head of the item's sequence (a copy of the last one beyond the end).
 struct Rows {
-  int token, head, pos;      // head: of Q
+  int token, head, pos;      // head: of Q; pos: the last key that it sees
   bool ok;
   int pos_first, pos_last;   // of the first and the last row, the same in all lanes
 };
@@ -264,17 +269,17 @@ __device__ __forceinline__ Rows rows_of(const PagedCall& c, const Sequence& s, i
   const int i = token_of(c, row);
   w.head = h * c.G + (row - i * c.G);
   w.token = s.first + i;
-  const int base = s.L - s.m, all = s.L - 1;
-  w.pos = c.causal ? base + i : all;
-  w.pos_first = __builtin_amdgcn_readfirstlane(c.causal ? base + token_of(c, min(row0, s.rows - 1)) : all);
-  w.pos_last = __builtin_amdgcn_readfirstlane(c.causal ? base + token_of(c, min(row0 + 31, s.rows - 1)) : all);
+  const int all = s.L - 1;
+  w.pos = c.causal ? min(s.base + i, all) : all;
+  w.pos_first = __builtin_amdgcn_readfirstlane(c.causal ? min(s.base + token_of(c, min(row0, s.rows - 1)), all) : all);
+  w.pos_last = __builtin_amdgcn_readfirstlane(c.causal ? min(s.base + token_of(c, min(row0 + 31, s.rows - 1)), all) : all);
   return w;
 }
 
 // Tiles of `keys` keys that block t sees: those of its last row.
 template <int BR> __device__ __forceinline__ int tiles_of(const PagedCall& c, const Sequence& s, int t, int keys) {
   const int last_row = min((t + 1) * BR, s.rows) - 1;
-  const int last = c.causal ? s.L - s.m + token_of(c, last_row) : s.L - 1;
+  const int last = c.causal ? min(s.base + token_of(c, last_row), s.L - 1) : s.L - 1;
   return last < 0 ? 0 : last / keys + 1;
 }
 // Where a cut at distance z of an item of length v falls among its tiles (the same for the pieces on both sides).

@@ -1,4 +1,6 @@
-"""Starts beyond what there is mean the same to the append and to the attention: a token has one position."""
+"""Lengths and starts beyond what there is mean the same to the append and to the attention: a token has one position."""
+import copy
+
 import pytest
 import torch
 
@@ -49,3 +51,26 @@ def test_starts_that_fall_write_no_row_behind_a_length():
         for c in (kc, vc):
             rows = c.view(3, 6, Hk, page, d).transpose(2, 3).reshape(3, 6 * page, Hk, d)
             assert all(bool((rows[b, n:] == 7.0).all()) for b, n in enumerate(lengths))
+
+
+@pytest.mark.parametrize("d,page", [(32, 16), (64, 32), (128, 16)])
+@pytest.mark.parametrize("new", [1, 20, 150])
+@pytest.mark.parametrize("over", [1, 9, 1000, 2 ** 30])
+def test_lengths_beyond_the_table(new, over, d, page):
+    """A length `over` tokens beyond what a row of the table holds, causal: token i stands at position length - new + i, as in the append, and sees the keys
+    up to its own that there are."""
+    capacity = 320
+    batch = ph.Batch([capacity - new, 100], [new, 3], 4, 2, d, "bf16", page, seed=d + new)
+    q, kc, vc, table, lengths, starts = batch.gpu()
+    lengths[0] += over
+    assert table.shape[1] * page == capacity
+    out, lse = binding.attn_paged_fwd(q, kc, vc, table, lengths, starts, softmax_scale=batch.tau)
+    # every token a sequence of its own, as long as it sees
+    plain = copy.copy(batch)
+    positions = [capacity + over - new + i for i in range(new)] + [100, 101, 102]
+    plain.B, plain.new, plain.starts = batch.tokens, [1] * batch.tokens, torch.arange(batch.tokens + 1)
+    plain.lengths = [min(p + 1, capacity) for p in positions]
+    plain.table = torch.cat([batch.table[:1].expand(new, -1), batch.table[1:].expand(3, -1)])
+    want, want_l, bound, bound_l = ph.attention(plain, True)
+    ph.assert_within(out, want, bound, "O")
+    ph.assert_within(lse, want_l, bound_l, "LSE")
