@@ -331,6 +331,7 @@ int attn_rotary(const attn_rotary_params* p, const attn_rotary_tensor* tensors, 
  *   query_starts   device int32 [B + 1], rising: rows query_starts[b] .. query_starts[b + 1] - 1 of the token tensors [T, heads, d] are the
  *                  new tokens of sequence b, its last ones.  NULL: row b is the one new token of sequence b (then T >= B).
  *                  Rows of no sequence (behind the last, in a padded batch) are not read, and are left as they were in the outputs.
+ *                  Starts that fall give unspecified outputs.
  * These three are read on the GPU only: a captured graph follows their contents.  Whatever they hold, nothing outside the tensors is
  * read or written: starts are forced into 0 .. T; a sequence has as many keys as its length says, but no more than a row of its table holds, table_width * page_size
  * (its new tokens keep the positions that its length gives them); and a page

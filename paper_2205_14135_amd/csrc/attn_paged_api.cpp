@@ -111,6 +111,8 @@ int check_paged(const attn_paged_params* p, attn::PagedCall* out, attn::PagedSha
   // the line that the work is laid out on (attn_paged_line.h), at its longest (320: what an item costs beside its keys, at most)
   const double rows = (double)p->T * c.G, blocks = rows / shape->rows + p->B;
   if (p->Hk * (blocks * c.G * ((double)c.b.capacity + 320) + rows * (blocks + 1)) > 0x1p50) return ATTN_ERR_SHAPE;
+  // (a sequence of r rows has at most r / BR + 1 blocks, and the sum over these of BR (t + 1) is at most (r + BR) (r / BR + 2) / 2: not above 2^51)
+  c.longest_line = p->Hk * (blocks * c.G * ((double)c.b.capacity + 320) + 0.5 * (rows + (double)p->B * shape->rows) * (rows / shape->rows + 2)) + 1;
   return ATTN_OK;
 }
 

@@ -223,8 +223,11 @@ template <class DIV> struct Work {
   // what there is to join.
   __device__ __forceinline__ bool begin(const PagedCall& c, const Numbers& numbers) {
     line.init(c, numbers);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *join_slots(c) = line.total == 0.0 ? 0 : line.n;
-    if (line.total == 0.0) return false;
+    // (starts that fall can give rows to several sequences, up to B T in all: what is longer than any line of rising starts is not begun, since its points need not be
+    // exact, its items need not exist, and its end may be hours away)
+    const bool some = line.total > 0.0 && line.total <= c.longest_line;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *join_slots(c) = some ? line.n : 0;
+    if (!some) return false;
     slot = xcd_item(line.n, (line.n + kXcds - 1) / kXcds);   // neighbours on the line share an XCD's L2
     if (slot < 0) return false;
     at = line.locate(c, line.start(slot), s);

@@ -74,3 +74,28 @@ def test_lengths_beyond_the_table(new, over, d, page):
     want, want_l, bound, bound_l = ph.attention(plain, True)
     ph.assert_within(out, want, bound, "O")
     ph.assert_within(lse, want_l, bound_l, "LSE")
+
+
+@pytest.mark.parametrize("T,d,Hq,Hk", [(64, 64, 8, 2), (2000, 64, 8, 2), (4000, 128, 4, 4)])
+def test_starts_that_share_rows_are_not_begun(T, d, Hq, Hk):
+    """Every second sequence would have all rows: many times the work of any rising starts."""
+    B, page, width = 64, 16, 40
+    q = torch.randn(T, Hq, d, device="cuda").to(torch.bfloat16)
+    kc, vc = (torch.randn(8, Hk, page, d, device="cuda").to(torch.bfloat16) for _ in range(2))
+    table, lengths = torch.zeros(B, width, dtype=torch.int32, device="cuda"), ints([page * width] * B)
+    out, lse = torch.full_like(q, 7.0), torch.full((Hq, T), 7.0, device="cuda")
+    for causal in (True, False):
+        binding.attn_paged_fwd(q, kc, vc, table, lengths, ints([0, T] * (B // 2) + [0]), softmax_scale=0.1, causal=causal, out=out, lse=lse)
+        assert bool((out == 7.0).all()) and bool((lse == 7.0).all())
+
+
+@pytest.mark.parametrize("B,width", [(1 << 16, 1024), (1 << 13, 512)])
+def test_starts_that_share_rows_beyond_what_doubles_hold(B, width):
+    """(2^57 and 2^51 units of work, where rising starts give 2^45 at most)"""
+    T, Hq, Hk, d, page = 1 << 16, 64, 8, 16, 4096
+    q = torch.zeros(T, Hq, d, dtype=torch.bfloat16, device="cuda")
+    kc, vc = (torch.zeros(1, Hk, page, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table, lengths = torch.zeros(1, width, dtype=torch.int32, device="cuda").expand(B, width), ints([page * width] * B)
+    out, lse = torch.full_like(q, 7.0), torch.full((Hq, T), 7.0, device="cuda")
+    binding.attn_paged_fwd(q, kc, vc, table, lengths, ints([0, T] * (B // 2) + [0]), softmax_scale=0.1, causal=False, out=out, lse=lse)
+    assert bool((out == 7.0).all()) and bool((lse == 7.0).all())
