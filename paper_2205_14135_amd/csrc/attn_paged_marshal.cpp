@@ -10,6 +10,8 @@
 #include <torch/csrc/autograd/saved_variable.h>
 #include <torch/csrc/autograd/variable.h>
 
+#include <mutex>
+
 namespace {
 
 using namespace marshal;
@@ -162,7 +164,13 @@ struct RotaryBackward : torch::autograd::Node {
   double magnitude = 1.0;
 
   variable_list apply(variable_list&& grads) override {
-    const Rotation r = {frequencies.unpack(), positions.unpack(), interleaved, !inverse, magnitude};
+    Rotation r = {at::Tensor(), at::Tensor(), interleaved, !inverse, magnitude};
+    {
+      // (another thread may run the same graph, and its engine let go of the saved tensors)
+      const std::lock_guard<std::mutex> lock(mutex_);
+      r.frequencies = frequencies.unpack();
+      r.positions = positions.unpack();
+    }
     const at::Tensor q = grads[0].defined() && should_compute_output(0) ? readable(grads[0]) : at::Tensor();
     const at::Tensor k = grads[1].defined() && should_compute_output(1) ? readable(grads[1]) : at::Tensor();
     const at::Tensor& x = q.defined() ? q : k;
@@ -176,6 +184,7 @@ struct RotaryBackward : torch::autograd::Node {
     return rotary_embedding(q, k, r);
   }
   void release_variables() override {
+    const std::lock_guard<std::mutex> lock(mutex_);
     frequencies.reset_data();
     positions.reset_data();
   }
