@@ -50,12 +50,15 @@ class _RotaryEmbedding(torch.autograd.Function):
     def forward(ctx, q, k, frequencies, interleaved, magnitude, positions, inverse):
         ctx.save_for_backward(frequencies, positions)
         ctx.kw = (interleaved, magnitude, inverse)
+        ctx.pairs = frequencies.shape
         return binding.attn_rotary(q, k, Rotary(frequencies, interleaved=interleaved, magnitude=magnitude), positions=positions, inverse=inverse)
 
     @staticmethod
     def backward(ctx, d_q, d_k):
         frequencies, positions = ctx.saved_tensors
         interleaved, magnitude, inverse = ctx.kw
+        if frequencies.shape != ctx.pairs:
+            raise ValueError("the saved frequencies or positions are not those of the forward call")
         return (*_RotaryEmbedding.apply(d_q.contiguous(), d_k.contiguous(), frequencies, interleaved, magnitude, positions, not inverse), None, None, None, None, None)
 
 

@@ -160,6 +160,7 @@ variable_list rotary_embedding(const at::Tensor& q, const at::Tensor& k, const R
 // of 1024 tokens took 75 us of host time.
 struct RotaryBackward : torch::autograd::Node {
   SavedVariable frequencies, positions;
+  int64_t pairs = 0;   // that turn
   bool interleaved = false, inverse = false;
   double magnitude = 1.0;
 
@@ -177,7 +178,7 @@ struct RotaryBackward : torch::autograd::Node {
     if (!x.defined()) return {at::Tensor(), at::Tensor()};
     // (hooks of the program may have handed back something else than what was saved)
     const at::Tensor &f = r.frequencies, &p = r.positions;
-    if (f.scalar_type() != at::kDouble || f.dim() != 1 || !f.is_contiguous() || f.device() != x.device() ||
+    if (f.scalar_type() != at::kDouble || f.dim() != 1 || f.size(0) != pairs || !f.is_contiguous() || f.device() != x.device() ||
         (p.defined() && (p.device() != x.device() || p.scalar_type() != at::kInt || (p.dim() == 1 ? p.size(0) != x.size(2) : p.dim() != 2 || p.size(0) != x.size(0) || p.size(1) != x.size(2)) ||
                          (x.size(2) > 1 && p.stride(p.dim() - 1) != 1))))
       refused_in_backward([] { raise(PyExc_ValueError, "the saved frequencies or positions are not those of the forward call"); });
@@ -205,6 +206,7 @@ variable_list rotary_embedding(const at::Tensor& q, const at::Tensor& k, const R
     node->set_next_edges(torch::autograd::collect_next_edges(q, k));
     node->frequencies = SavedVariable(r.frequencies, false);
     node->positions = SavedVariable(r.positions, false);
+    node->pairs = r.frequencies.size(0);
     node->interleaved = r.interleaved;
     node->inverse = r.inverse;
     node->magnitude = r.magnitude;

@@ -130,6 +130,20 @@ def test_saved_tensors_that_come_back_changed(change):
         torch.autograd.grad(ys, (q, k), (gq, gk))
 
 
+@pytest.mark.parametrize("python_node", [False, True])
+def test_saved_frequencies_that_come_back_in_another_number(python_node, monkeypatch):
+    """(fewer or more columns would turn than did)"""
+    from paper_2205_14135_amd import autograd
+    if python_node:
+        monkeypatch.setattr(autograd, "_node_in_python", lambda: True)
+    q, k, gq, gk, _, _ = _tensors()
+    for change in (lambda x: x[:3], lambda x: torch.cat([x, x])):
+        with torch.autograd.graph.saved_tensors_hooks(lambda x: x, change):
+            ys = rotary_embedding(q, k, Rotary.make(32))
+        with pytest.raises(ValueError, match="saved frequencies or positions"):
+            torch.autograd.grad(ys, (q, k), (gq, gk))
+
+
 def test_transforms_keep_the_python_node():
     q, k, gq, _, rotary, pos = _tensors(False)
     with pytest.raises(RuntimeError, match="setup_context"):
