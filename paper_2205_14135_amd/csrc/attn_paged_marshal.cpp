@@ -11,6 +11,8 @@
 #include <torch/csrc/autograd/variable.h>
 
 #include <mutex>
+#include <unordered_set>
+#include <vector>
 
 namespace {
 
@@ -220,18 +222,28 @@ variable_list rotary_embedding(const at::Tensor& q, const at::Tensor& k, const R
 }
 
 // The node that sums a leaf's gradient lives as long as any graph that leads to the leaf, and keeps the stream it was made on.  A captured backward pass that meets one of the
-// default stream makes that stream wait for the capture, which ends the process; so the forward pass refuses.
-void refuse_eager_graphs(std::initializer_list<const at::Tensor*> leaves) {
+// default stream makes that stream wait for the capture, which ends the process; so the forward pass refuses.  In a model the leaves are weights, behind other operations: all
+// nodes that a backward pass from these tensors reaches are looked at (under capture alone: once in the life of a graph).
+void refuse_eager_graphs(std::initializer_list<const at::Tensor*> tensors) {
+  using torch::autograd::Node;
   if (c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None) return;
-  for (const at::Tensor* t : leaves) {
-    if (!t->defined() || !t->is_leaf() || !t->requires_grad()) continue;
-    const std::shared_ptr<torch::autograd::Node> sum = torch::autograd::impl::try_get_grad_accumulator(*t);
-    if (sum != nullptr && sum->stream().has_value() && sum->stream()->id() == 0)
+  std::vector<std::shared_ptr<Node>> todo;
+  std::unordered_set<const Node*> seen;
+  for (const at::Tensor* t : tensors) {
+    if (!t->defined() || !t->requires_grad()) continue;
+    todo.push_back(t->is_leaf() ? torch::autograd::impl::try_get_grad_accumulator(*t) : t->grad_fn());
+  }
+  while (!todo.empty()) {
+    const std::shared_ptr<Node> node = std::move(todo.back());
+    todo.pop_back();
+    if (node == nullptr || !seen.insert(node.get()).second) continue;
+    if (node->stream().has_value() && node->stream()->id() == 0)
       raise(PyExc_RuntimeError, "captured while a graph made on the default stream still leads to the same leaf: drop that graph (its outputs) first, or make it on another stream");
+    for (const torch::autograd::Edge& e : node->next_edges()) todo.push_back(e.function);
   }
 }
 
-// rotary_embedding(Q, K, frequencies, interleaved, magnitude, positions, V) -> (Q', K'), differentiable.  V: a leaf of the same pass, or None.
+// rotary_embedding(Q, K, frequencies, interleaved, magnitude, positions, V) -> (Q', K'), differentiable.  V: of the same pass, or None.
 PyObject* py_rotary_embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
     expect_args(n, 7);
