@@ -62,11 +62,19 @@ void expect_gpu(const at::Tensor& ref, std::initializer_list<const at::Tensor*> 
 at::Tensor maybe(PyObject* o) { return o == Py_None ? at::Tensor() : tensor(o); }
 const void* ptr(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 
-// An output with the strides of what it comes from, so that Q and K keep V's; packed where the input repeats rows.
+// An output with the strides of what it comes from, so that Q and K keep V's (the attention takes three tensors of the same strides); packed where the input repeats rows.
 at::Tensor output_like(const at::Tensor& x) {
   for (int64_t i = 0; i + 1 < x.dim(); ++i)
     if (x.size(i) > 1 && x.stride(i) == 0) return at::empty(x.sizes(), x.options());
   return at::empty_strided(x.sizes(), x.strides(), x.options());
+}
+
+// An output that need not share strides with anything: in its input's order of axes, without the input's gaps (Q may be a part of a projection's rows, or one
+// token's of a long tensor).
+at::Tensor packed_like(const at::Tensor& x) {
+  for (int64_t i = 0; i + 1 < x.dim(); ++i)
+    if (x.size(i) > 1 && x.stride(i) == 0) return at::empty(x.sizes(), x.options());
+  return at::empty_like(x, x.options(), at::MemoryFormat::Preserve);
 }
 
 int32_t narrow(int64_t v) { return v > INT32_MAX ? -1 : (int32_t)v; }   // (the library refuses what is negative)
@@ -155,7 +163,7 @@ at::Tensor readable(const at::Tensor& t) {
   return ok ? t : t.clone(at::MemoryFormat::Contiguous);
 }
 
-variable_list rotary_embedding(const at::Tensor& q, const at::Tensor& k, const Rotation& r);
+variable_list rotary_embedding(const at::Tensor& q, const at::Tensor& k, const Rotation& r, at::Tensor (*make)(const at::Tensor&));
 
 // The gradient of a rotation is the rotation by the negative angle, with a node of the same kind where it is to be differentiated again.  A node of its own class, with
 // its fields as members: with a torch::autograd::Function (its context keeps them in a dictionary by name) a forward and backward of 8 x 16 heads
@@ -184,7 +192,7 @@ struct RotaryBackward : torch::autograd::Node {
         (p.defined() && (p.device() != x.device() || p.scalar_type() != at::kInt || (p.dim() == 1 ? p.size(0) != x.size(2) : p.dim() != 2 || p.size(0) != x.size(0) || p.size(1) != x.size(2)) ||
                          (x.size(2) > 1 && p.stride(p.dim() - 1) != 1))))
       refused_in_backward([] { raise(PyExc_ValueError, "the saved frequencies or positions are not those of the forward call"); });
-    return rotary_embedding(q, k, r);
+    return rotary_embedding(q, k, r, packed_like);
   }
   void release_variables() override {
     const std::lock_guard<std::mutex> lock(mutex_);
@@ -194,13 +202,13 @@ struct RotaryBackward : torch::autograd::Node {
   std::string name() const override { return "RotaryBackward"; }
 };
 
-// q or k may be undefined.  Called without the interpreter lock.
-variable_list rotary_embedding(const at::Tensor& q, const at::Tensor& k, const Rotation& r) {
+// q or k may be undefined; make: their outputs.  Called without the interpreter lock.
+variable_list rotary_embedding(const at::Tensor& q, const at::Tensor& k, const Rotation& r, at::Tensor (*make)(const at::Tensor&)) {
   const at::Tensor& x = q.defined() ? q : k;
   const c10::DeviceGuard guard(x.device());
   at::Tensor qo, ko;
-  if (q.defined()) qo = output_like(q);
-  if (k.defined()) ko = output_like(k);
+  if (q.defined()) qo = make(q);
+  if (k.defined()) ko = make(k);
   const int status = q.defined() ? rotate(q, k, qo, ko, r) : rotate(k, q, ko, qo, r);
   if (status != ATTN_OK) refused_in_backward([&] { check_status(status, "attn_rotary"); });
   if (torch::autograd::compute_requires_grad(q, k)) {
@@ -258,7 +266,7 @@ PyObject* py_rotary_embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
     {
       PyThreadState* const s = PyEval_SaveThread();
       try {
-        out = rotary_embedding(q, k, r);
+        out = rotary_embedding(q, k, r, output_like);
       } catch (...) {
         PyEval_RestoreThread(s);
         throw;
@@ -345,7 +353,7 @@ PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const c10::DeviceGuard guard(k.device());
     p.stream = current_stream(k);
     if (q.defined()) {
-      if (!out.defined()) out = output_like(q);
+      if (!out.defined()) out = packed_like(q);
       p.Hq = narrow(q.size(1));
       p.q_stride_t = axis_stride(q, 0); p.q_stride_h = axis_stride(q, 1); p.o_stride_t = axis_stride(out, 0); p.o_stride_h = axis_stride(out, 1);
     }
@@ -377,7 +385,7 @@ PyObject* py_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     expect_gpu(q, b, {&out, &lse, &ws});
     const c10::DeviceGuard guard(q.device());
     p.stream = current_stream(q);
-    if (!out.defined()) out = output_like(q);
+    if (!out.defined()) out = packed_like(q);
     if (!lse.defined()) lse = at::empty({q.size(1), q.size(0)}, q.options().dtype(at::kFloat));
     p.q_stride_t = axis_stride(q, 0); p.q_stride_h = axis_stride(q, 1); p.o_stride_t = axis_stride(out, 0); p.o_stride_h = axis_stride(out, 1);
     if (!ws.defined()) ws = at::empty({(int64_t)std::max<size_t>(lib.workspace_bytes(&p), 256)}, q.options().dtype(at::kByte));

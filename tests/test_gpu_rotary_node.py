@@ -96,6 +96,17 @@ def test_backward_from_two_threads():
             assert all(torch.equal(a, b) for a, b in zip(g, want))
 
 
+def test_gradients_have_no_gaps():
+    """Gradients with the strides of a projection's part, as the attention hands them back: what comes out holds its own elements alone."""
+    q, k, gq, gk, rotary, pos = _tensors()
+    wide = [torch.zeros(2, 40, 3 * g.shape[1], 64, dtype=g.dtype, device="cuda")[:, :, :g.shape[1]].transpose(1, 2).copy_(g) for g in (gq, gk)]
+    ys = rotary_embedding(q, k, rotary, pos)
+    want = torch.autograd.grad(ys, (q, k), (gq, gk), retain_graph=True)
+    got = torch.autograd.grad(ys, (q, k), wide)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert all(g.untyped_storage().nbytes() == 2 * g.numel() for g in got)
+
+
 def test_saved_tensor_hooks_and_checkpoint():
     q, k, gq, gk, rotary, pos = _tensors()
     want = torch.autograd.grad(rotary_embedding(q, k, rotary, pos), (q, k), (gq, gk))
