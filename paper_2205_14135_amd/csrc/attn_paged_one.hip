@@ -13,7 +13,8 @@
 namespace attn {
 namespace {
 
-// (cuts moved by up to 48 keys or 64 instead of 32: single tokens of mixed lengths 1 and 3 per cent slower)
+// (cuts moved by up to 48 keys or 64 instead of 32: single tokens of mixed lengths 1 and 3 per cent slower.  SPREAD, us with the join, 0 | 1 | 4 | 16: one token on 30000, 4 heads of 64, 30.0 | 20.5 |
+// 19.8 | 26.1, on 4000 10.6 | 10.6 | 11.0 | 14.1, 8 heads of 128 15.7 | 15.4 | 17.0 | 20.2; two on 10^5 and 64 of 128 to 8192 the same with all four.)
 typedef Division<32, 32, 64, 32, 1> Div;
 constexpr int BR = Div::BR;
 
@@ -28,6 +29,8 @@ template <int D> struct OneShape {
 
 // Online softmax of a tile of 32 NB keys, lane = row (two lanes a row): as softmax_tile_lane_query in attn_common.h, but the reference follows the maximum of every tile,
 // and the sum of the rounded probabilities is taken on the vector unit, which is idle here.
+// Probabilities are rounded to 16 bits, half a step each, because the matrix unit takes the product with V in 16 bits, as in the dense forward; O is divided by the sum of the rounded
+// ones, so that weights still sum to 1, and maxima, sums, pieces and joins are in 32 bits.  O is off by 0.0020 to 0.0023 of its norm in bf16, 0.0017 with 32-bit weights rounded once at the end.
 template <typename T, int DB, int NB>
 __device__ __forceinline__ void softmax_tile(f32x16 (&st)[NB], f32x16 (&o)[DB], typename Vec<T>::x8 (&pf)[2 * NB], float& m_run, float& l_run, float& lr_run, float cs, int k0,
                                              const Rows& w, int L, int g) {

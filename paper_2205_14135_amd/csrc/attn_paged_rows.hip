@@ -10,7 +10,8 @@
 // ahead: the address of a copy is scalar work alone.  (One load a tile, used in the next, makes the compiler wait for the copies issued since: its count
 // of loads in flight does not know them.)
 //   The stretches of the line (attn_paged_line.h) make up for blocks of unequal length, short batches and single tokens in between.  Rates, 16 heads, against the dense
-// forward without pages: d = 128, 2 x 8192 not causal 1130 TFLOP/s, 97 % of it, causal 990, 90 %; d = 64, 870, 101 %, and 797, 88 %.  What the causal batches lose is the start and the end of stretches.
+// forward without pages, pages of 16 in any order | of 256: d = 128, 2 x 8192 not causal 1160 TFLOP/s, 97 % of it | 97 %, causal 980, 87 % | 92 %; d = 64, 820, 95 % | 103 %, and 810, 87 % | 88 %.  What the
+// causal batches lose is the start and the end of stretches.
 #include "attn_paged_line.h"
 
 namespace attn {
@@ -18,6 +19,8 @@ namespace {
 
 // us, ITEM and SLACK of 256 and 160 | 320 and 320, 128 and 96 | 256 and 256, 16 heads: d = 128, 8 x 256 tokens 25 | 18, 8 x 1024 67 | 67; d = 64, 8 x 256 22 | 14, 32 x 64 on 100 20 | 13, 4 x 4096
 // 195 | 195.  Over 76 batches, 32 of them ragged, the same within 1 per cent at d = 128, 6 to 8 less at d = 64; 25 per cent more or less of either changes nothing.
+// SPREAD, us with the join, 4 | 18 | 72 | 288: d = 64, 4 heads, 128 tokens on 60000 65 | 65 | 62 | 76; d = 128, 8 heads, 8 x 16 on 2000 22 | 22 | 22 | 29, 256 on 60000 237 | 240 | 238 | 241, 2048 on 14336 and
+// 8 x 256 the same with all four: anything between 4 and 72 will do.
 typedef Division<256, 64, 320, 320, 18> PairDiv;    // two groups of four wavefronts
 typedef Division<128, 64, 256, 256, 18> BlockDiv;   // four wavefronts
 constexpr int BC = 64;

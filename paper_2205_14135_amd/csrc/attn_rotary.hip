@@ -20,7 +20,8 @@ constexpr int NT = 256;
 // How the columns of a unit u (of d / 16) pair up.
 //   kHalves (r a multiple of 16): 8 columns from 8 u on and the 8 that lie r / 2 behind; behind the turning columns, 16 in a row
 //   kNeighbours: columns 16 u .. 16 u + 15, pairs inside
-//   kHalvesAny: the same columns, each partner read by itself
+//   kHalvesAny: the same columns, each partner read by itself: sixteen loads of two bytes a thread and head bound it.  128 MiB of Q and K in and out, d = 64, r = 20: 72 us
+//   (1.9 TB/s), r = 6 at d = 16 69, where kHalves takes 23 to 25 and kNeighbours 24 to 25 (5.3 to 5.8 TB/s)
 enum Pairing { kHalves, kNeighbours, kHalvesAny };
 
 // cosine and sine, times the factor, of the angle at `position` of pair i (of no use behind the last)
@@ -238,8 +239,9 @@ __global__ __launch_bounds__(NT) void append_kernel(const AppendCall c, const in
   }
 }
 
-// Heads a thread walks over: as many as leave 8 wavefronts a SIMD's worth of threads (its angles are then computed once for all of them), at most 8; and at least so many
-// that a grid's second axis holds the rest.
+// Heads a thread walks over: as many as leave 8 wavefronts to a compute unit (its angles are then computed once for all of them), at most 8; and at least so many
+// that a grid's second axis holds the rest.  us, 8 wavefronts | 32: 8 x 1024 tokens of 16 + 16 heads of 64 13.0 | 15.1, 4 x 2048 of 8 + 8 heads of 32 6.2 | 7.6, 197 of 12 + 12 of 64 4.4 | 4.4,
+// 16384 of 16 + 4 of 128 29.8 | 29.7.
 int heads_per_thread(int64_t token_units, int heads) {
   const int64_t enough = (int64_t)kComputeUnits * 8 * 64;
   int per = 8;
