@@ -296,7 +296,7 @@ typedef struct {
 } attn_rotary_spec;
 
 /* A [B,H,N,d] tensor and where its turned copy goes (y == x with the same strides: in place).  Strides in elements, multiples of 8, the d axis
- * contiguous; pointers 16-byte aligned.  x and y must not overlap otherwise. */
+ * contiguous; pointers 16-byte aligned.  x and y must not overlap otherwise, nor y and what the call's other tensor reads or writes. */
 typedef struct {
   const void* x;
   void* y;
@@ -358,7 +358,8 @@ typedef struct {
 
 /*
  * Writes the new tokens' K and V rows into the pages, token i of the m new ones of sequence b at position lengths[b] - m + i (a position that is negative, or behind
- * the table's last page, is not written).  Where the table gives two tokens of a call the same row, one of them is what stands there.  With rotary != NULL K is turned by its position, and so is Q, if one is given, into Qout (in place where
+ * the table's last page, is not written).  Where the table gives two tokens of a call the same row, every 16 bytes of it are one or the other's.  What is
+ * written must not overlap what else the call reads or writes.  With rotary != NULL K is turned by its position, and so is Q, if one is given, into Qout (in place where
  * Qout == Q with the same strides).  rotary == NULL: K is copied; then Q must be NULL.
  */
 int attn_paged_append(const attn_paged_params* p, const attn_rotary_spec* rotary, const void* K, const void* V, void* k_cache, void* v_cache, const void* Q,

@@ -141,6 +141,8 @@ int attn_rotary(const attn_rotary_params* p, const attn_rotary_tensor* tensors, 
     if (t.x == t.y && (xb.stride != yb.stride || xh.stride != yh.stride || xn.stride != yn.stride)) return ATTN_ERR_SHAPE;
     c.t[i] = {t.x, t.y, t.H, xb.stride, xh.stride, xn.stride, yb.stride, yh.stride, yn.stride};
   }
+  // (what one tensor's threads write, the other's must not read or write)
+  if (n_tensors == 2 && (tensors[0].y == tensors[1].y || tensors[0].y == tensors[1].x || tensors[1].y == tensors[0].x)) return ATTN_ERR_SHAPE;
   c.n_tensors = n_tensors;
   c.B = p->B; c.N = p->N; c.d = p->d;
   c.positions = p->positions;
@@ -173,6 +175,8 @@ int attn_paged_append(const attn_paged_params* p, const attn_rotary_spec* rotary
     if (Q == Qout && (qt.stride != ot.stride || qh.stride != oh.stride)) return ATTN_ERR_SHAPE;
     c.qt = qt.stride; c.qh = qh.stride; c.ot = ot.stride; c.oh = oh.stride;
   }
+  // (what two groups of threads would write, or one write and the other read)
+  if (k_cache == v_cache || (Q != nullptr && (Qout == K || Qout == V || Qout == k_cache || Qout == v_cache))) return ATTN_ERR_SHAPE;
   c.d = p->d;
   c.K = K; c.V = V; c.Q = Q; c.Kc = k_cache; c.Vc = v_cache; c.Qo = Qout;
   c.kt = kt.stride; c.kh = kh.stride; c.vt = vt.stride; c.vh = vh.stride;
