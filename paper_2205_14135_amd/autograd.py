@@ -73,8 +73,9 @@ def rotary_embedding(q: torch.Tensor, k: torch.Tensor, rotary: Rotary, positions
     """(q', k'): q and k turned by their tokens' positions, differentiable with respect to both (any number of times).
 
     q, k: [B,H,N,d] fp16 or bf16 CUDA tensors, d contiguous, d in {16, 32, 64, 128}; their numbers of heads and strides may differ.  positions:
-    int32 [N] or [B,N] (default 0 .. N - 1).  The frequencies get no gradient: such as require one are refused.  One launch forward, one backward.  In a captured graph that holds the backward pass too, no eager graph may lead to the same
-    leaves any more (drop its outputs first): a forward pass that meets one of the default stream is refused.
+    int32 [N] or [B,N] (default 0 .. N - 1).  The frequencies get no gradient: such as require one are refused.  One launch forward, one backward.
+    In a captured graph that holds the backward pass too, no eager graph may lead to the same leaves any more, directly or through other operations
+    (drop its outputs first): a forward pass that meets one of the default stream is refused.
     """
     return _turned(q, k, None, rotary, positions)
 
