@@ -78,7 +78,9 @@ typedef enum {
   ATTN_ERR_MASK = -8,       /* mask_block != 128 or negative mask stride */
   ATTN_ERR_LAUNCH = -9,     /* the HIP runtime refused the launch */
   ATTN_ERR_PAGES = -10,     /* page size no power of two in [16, 4096], or a list of page copies that names a page it must not */
-  ATTN_ERR_ROTARY = -11     /* rotary_dim odd or not in [2, d], no frequencies, or a factor that is not finite */
+  ATTN_ERR_ROTARY = -11,    /* rotary_dim odd or not in [2, d], no frequencies, or a factor that is not finite */
+  ATTN_ERR_NORM = -12,      /* no weights, weights that are not aligned to their type, or eps not finite and > 0 */
+  ATTN_ERR_WINDOW = -13     /* window < 1, sinks < 0, or not causal */
 } attn_status;
 
 enum { ATTN_FP16 = 0, ATTN_BF16 = 1 };
@@ -322,6 +324,43 @@ typedef struct {
  */
 int attn_rotary(const attn_rotary_params* p, const attn_rotary_tensor* tensors, int32_t n_tensors);
 
+/* The norm of every row of Q and K: y = w o x / sqrt(mean(x^2) + eps), with one vector of weights for all heads of a tensor. */
+typedef struct {
+  const void* q_weight;        /* device, [d]: of the first tensor of a call                                */
+  const void* k_weight;        /* device, [d]: of the second                                                */
+  int32_t weights_fp32;        /* != 0: float32, else of the tensors' dtype                                 */
+  float eps;                   /* finite, > 0                                                               */
+} attn_norm_spec;
+
+/*
+ * Every row normed, then turned as by attn_rotary, in one pass and with one rounding.  p->rotary.frequencies == NULL with rotary_dim 0: the norm alone.  p->inverse must be 0.
+ * Sums are in 32 bits: a row whose squares add up beyond their range (elements near 10^18 in bf16) comes out as zeros.
+ */
+int attn_norm_rotary(const attn_rotary_params* p, const attn_norm_spec* norm, const attn_rotary_tensor* tensors, int32_t n_tensors);
+
+/* A tensor of its backward pass: x as the forward call read it, dy the gradient of what that wrote, both in; dx and the weights' gradient dw ([d], of the weights' type, NULL: not
+ * asked for) out.  Strides as in attn_rotary_tensor.  dx must not overlap what the call reads. */
+typedef struct {
+  const void* x;
+  const void* dy;
+  void* dx;
+  void* dw;
+  int32_t H;
+  int64_t x_stride_b, x_stride_h, x_stride_n;
+  int64_t dy_stride_b, dy_stride_h, dy_stride_n;
+  int64_t dx_stride_b, dx_stride_h, dx_stride_n;
+} attn_norm_grad;
+
+/* Bytes of scratch for attn_norm_rotary_bwd at head dimension d; 0 if there is none such. */
+size_t attn_norm_rotary_bwd_workspace_bytes(int32_t d);
+
+/*
+ * With g = dy turned back and h = g o w:  dx = r (h - x r^2 mean(h o x)),  dw = the sum over all rows of g o x r,  r = 1 / sqrt(mean(x^2) + eps).
+ * p and norm as in the forward call.  workspace: 256-byte aligned; contents on entry are ignored.  The same inputs give the same bits in every call.
+ */
+int attn_norm_rotary_bwd(const attn_rotary_params* p, const attn_norm_spec* norm, const attn_norm_grad* tensors, int32_t n_tensors, void* workspace,
+                         size_t workspace_bytes);
+
 /*
  * A batch of B sequences whose keys and values lie in the pages of a cache.
  *   caches         K and V: [pages, Hk, page_size, d], strides shared by both (multiples of 8 elements, d contiguous); page_stride and
@@ -364,6 +403,10 @@ typedef struct {
  */
 int attn_paged_append(const attn_paged_params* p, const attn_rotary_spec* rotary, const void* K, const void* V, void* k_cache, void* v_cache, const void* Q,
                       void* Qout);
+
+/* The same with Q and K normed first, Q with q_weight and K with k_weight (attn_norm_rotary).  rotary == NULL: the norm alone, of Q too if one is given. */
+int attn_paged_norm_append(const attn_paged_params* p, const attn_rotary_spec* rotary, const attn_norm_spec* norm, const void* K, const void* V, void* k_cache,
+                           void* v_cache, const void* Q, void* Qout);
 
 /* Bytes of scratch for attn_paged_fwd with these params.  The head dimension alone decides: a workspace serves every call at its head dimension.  0 if the params
  * are invalid. */

@@ -13,9 +13,10 @@ from typing import Optional
 
 import torch
 from torch.autograd import forward_ad
+from torch.autograd.function import once_differentiable
 
 from . import binding
-from .rotary import Rotary
+from .rotary import HeadNorm, Rotary
 
 
 class _FlashAttention(torch.autograd.Function):
@@ -62,6 +63,24 @@ class _RotaryEmbedding(torch.autograd.Function):
         return (*_RotaryEmbedding.apply(d_q.contiguous(), d_k.contiguous(), frequencies, interleaved, magnitude, positions, not inverse), None, None, None, None, None)
 
 
+class _NormRotaryEmbedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, eps, frequencies, interleaved, magnitude, positions):
+        ctx.save_for_backward(q, k, q_weight, k_weight, frequencies, positions)
+        ctx.kw = (eps, interleaved, magnitude)
+        rotary = None if frequencies is None else Rotary(frequencies, interleaved=interleaved, magnitude=magnitude)
+        return binding.attn_norm_rotary(q, k, HeadNorm(q_weight, k_weight, eps=eps), rotary, positions=positions)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, d_q, d_k):
+        q, k, q_weight, k_weight, frequencies, positions = ctx.saved_tensors
+        eps, interleaved, magnitude = ctx.kw
+        rotary = None if frequencies is None else Rotary(frequencies, interleaved=interleaved, magnitude=magnitude)
+        grads = binding.attn_norm_rotary_bwd(q, k, d_q.contiguous(), d_k.contiguous(), HeadNorm(q_weight, k_weight, eps=eps), rotary, positions=positions)
+        return (*grads, None, None, None, None, None)
+
+
 def _node_in_python() -> bool:
     # The nodes in Python stay for what has rules of its own for functions written in Python: functorch's transforms, forward-mode
     # differentiation, tracing and compilation.
@@ -90,11 +109,34 @@ def _turned(q, k, v, rotary, positions):
     return binding._marshal.rotary_embedding(q, k, rotary.frequencies, rotary.interleaved, rotary.magnitude, positions, v)
 
 
+def norm_rotary_embedding(q: torch.Tensor, k: torch.Tensor, norm: HeadNorm, rotary: Optional[Rotary] = None, positions: Optional[torch.Tensor] = None):
+    """(q', k'): every row of q and k normed (weight * x / sqrt(mean(x^2) + eps), `rotary.HeadNorm`), then turned by its token's position as by `rotary_embedding`, in one
+    pass; differentiable with respect to q, k and the weights, once.
+
+    Tensors and positions as in `rotary_embedding`, and its rule for captured graphs; rotary = None: the norm alone.  One launch forward, two backward (one if neither weight
+    asks for a gradient).
+    """
+    return _normed(q, k, None, norm, rotary, positions)
+
+
+def _normed(q, k, v, norm, rotary, positions):
+    if binding._lib is None:
+        binding.load()
+    if norm.k_weight is None:
+        raise ValueError("the norm has no weights for a tensor that is given")
+    f, i, m = binding._rotation(rotary)
+    if f is not None and f.requires_grad and torch.is_grad_enabled():
+        raise ValueError("the frequencies require a gradient, and there is none for them: detach them")
+    if _node_in_python():
+        return _NormRotaryEmbedding.apply(q, k, norm.q_weight, norm.k_weight, norm.eps, f, i, m, positions)
+    return binding._marshal.norm_rotary_embedding(q, k, norm.q_weight, norm.k_weight, norm.eps, f, i, m, positions, v)
+
+
 def flash_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, softmax_scale: Optional[float] = None,
                     causal: bool = False, dropout_p: float = 0.0, seed: Optional[int] = None, offset: int = 0,
                     key_lengths: Optional[torch.Tensor] = None,
                     block_mask: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
-                    positions: Optional[torch.Tensor] = None) -> torch.Tensor:
+                    positions: Optional[torch.Tensor] = None, norm: Optional[HeadNorm] = None) -> torch.Tensor:
     """softmax(scale * q k^T + mask) v with dropout on the probabilities; exact attention.
 
     q, k, v: [B,H,N,d] fp16 or bf16 CUDA tensors with identical shape and strides, d contiguous,
@@ -102,7 +144,7 @@ def flash_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, softma
     (key-padding mask).  block_mask: uint8 [T,T] or [H,T,T] over 128 x 128 blocks (then N % 128 == 0).
     With dropout_p > 0 the mask is a pure function of (seed, offset, b, h, i, j); seed defaults to a
     draw from torch's CPU generator, so torch.manual_seed makes a run reproducible.  With `rotary`, q and k are
-    turned by their `positions` first (`rotary_embedding`).
+    turned by their `positions` first (`rotary_embedding`), with `norm` their rows are normed before that, in the same pass (`norm_rotary_embedding`).
     """
     if not (q.is_cuda and k.is_cuda and v.is_cuda):
         raise RuntimeError("flash_attention runs on the GPU only: there is no CPU path")
@@ -112,7 +154,9 @@ def flash_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, softma
         seed = int(torch.randint(0, 2 ** 62, (), dtype=torch.int64).item())
     if binding._lib is None:
         binding.load()
-    if rotary is not None:
+    if norm is not None:
+        q, k = _normed(q, k, v, norm, rotary, positions)
+    elif rotary is not None:
         q, k = _turned(q, k, v, rotary, positions)
     elif positions is not None:
         raise ValueError("positions are of no use without rotary")

@@ -24,6 +24,7 @@ SYMBOLS = (
     "attn_fwd", "attn_bwd_workspace_bytes", "attn_blocksparse_bwd_workspace_bytes", "attn_bwd", "attn_bwd_static", "attn_blocksparse_fwd",
     "attn_blocksparse_bwd", "attn_bwd_timed", "attn_debug_dropout_mask", "attn_debug_mfma_rate", "attn_debug_kernel_choice", "attn_debug_bwd_kernel", "attn_debug_set_variant", "attn_strerror",
     "attn_version", "attn_rotary", "attn_paged_append", "attn_paged_workspace_bytes", "attn_paged_fwd", "attn_paged_copy",
+    "attn_norm_rotary", "attn_norm_rotary_bwd_workspace_bytes", "attn_norm_rotary_bwd", "attn_paged_norm_append",
 )
 
 
@@ -54,6 +55,15 @@ class RotaryTensor(ctypes.Structure):
 class RotaryParams(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("N", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rotary", RotarySpec),
                 ("inverse", ctypes.c_int32), ("positions", ctypes.c_void_p), ("position_stride_b", ctypes.c_int64), ("stream", ctypes.c_void_p)]
+
+
+class NormSpec(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("weights_fp32", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class NormGrad(ctypes.Structure):
+    _fields_ = [*[(n, ctypes.c_void_p) for n in ("x", "dy", "dx", "dw")], ("H", ctypes.c_int32),
+                *[(f"{t}_stride_{a}", ctypes.c_int64) for t in ("x", "dy", "dx") for a in "bhn"]]
 
 
 class PagedParams(ctypes.Structure):
@@ -100,6 +110,8 @@ def _attach_paged(lib: ctypes.CDLL) -> None:
     """The same for the rotary positions and the paged cache."""
     _marshal.attach_paged(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
         "attn_rotary", "attn_paged_append", "attn_paged_workspace_bytes", "attn_paged_fwd", "attn_paged_copy")))
+    _marshal.attach_norm(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
+        "attn_norm_rotary", "attn_norm_rotary_bwd_workspace_bytes", "attn_norm_rotary_bwd", "attn_paged_norm_append")))
 
 
 def load() -> ctypes.CDLL:
@@ -150,6 +162,14 @@ def load() -> ctypes.CDLL:
     lib.attn_paged_fwd.restype = ctypes.c_int
     lib.attn_paged_copy.argtypes = [ctypes.POINTER(PagedCopyParams), vp, vp, vp, i64]
     lib.attn_paged_copy.restype = ctypes.c_int
+    lib.attn_norm_rotary.argtypes = [ctypes.POINTER(RotaryParams), ctypes.POINTER(NormSpec), ctypes.POINTER(RotaryTensor), i32]
+    lib.attn_norm_rotary.restype = ctypes.c_int
+    lib.attn_norm_rotary_bwd_workspace_bytes.argtypes = [i32]
+    lib.attn_norm_rotary_bwd_workspace_bytes.restype = sz
+    lib.attn_norm_rotary_bwd.argtypes = [ctypes.POINTER(RotaryParams), ctypes.POINTER(NormSpec), ctypes.POINTER(NormGrad), i32, vp, sz]
+    lib.attn_norm_rotary_bwd.restype = ctypes.c_int
+    lib.attn_paged_norm_append.argtypes = [ctypes.POINTER(PagedParams), ctypes.POINTER(RotarySpec), ctypes.POINTER(NormSpec)] + [vp] * 6
+    lib.attn_paged_norm_append.restype = ctypes.c_int
     lib.attn_strerror.argtypes = [ctypes.c_int]
     lib.attn_strerror.restype = ctypes.c_char_p
     lib.attn_version.argtypes = []
@@ -326,16 +346,47 @@ def attn_rotary(Q, K, rotary, *, positions=None, inverse=False, out=None) -> Tup
     return _marshal.rotary(Q, K, rotary.frequencies, rotary.interleaved, rotary.magnitude, positions, inverse, q_out, k_out)
 
 
-def attn_paged_append(K, V, k_cache, v_cache, block_table, lengths, query_starts=None, *, Q=None, rotary=None, out=None) -> Optional[torch.Tensor]:
+def _rotation(rotary):
+    return (None, False, 1.0) if rotary is None else (rotary.frequencies, rotary.interleaved, rotary.magnitude)
+
+
+def attn_norm_rotary(Q, K, norm, rotary=None, *, positions=None, out=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Q and K (or Q alone: K = None), every row normed (norm: a `rotary.HeadNorm`) and then turned by its position as in attn_rotary, in one launch.
+
+    rotary: None for the norm alone.  The other arguments are those of attn_rotary."""
+    if _lib is None:
+        load()
+    q_out, k_out = (None, None) if out is None else out
+    return _marshal.norm_rotary(Q, K, norm.q_weight, norm.k_weight, norm.eps, *_rotation(rotary), positions, q_out, k_out)
+
+
+def attn_norm_rotary_bwd(Q, K, dQ_out, dK_out, norm, rotary=None, *, positions=None, workspace=None):
+    """dQ, dK, dq_weight, dk_weight from Q and K as attn_norm_rotary read them and the gradients of what it returned (K = dK_out = None: Q alone).
+
+    The gradients of the weights are sums over all rows, in 32 bits and in a fixed order.  workspace: attn_norm_rotary_bwd_workspace_bytes(d) bytes, made here unless
+    given.  Runs on torch's current stream."""
+    if _lib is None:
+        load()
+    return _marshal.norm_rotary_bwd(Q, K, dQ_out, dK_out, norm.q_weight, norm.k_weight, norm.eps, *_rotation(rotary), positions, workspace)
+
+
+def attn_norm_rotary_bwd_workspace_bytes(d: int) -> int:
+    return int(load().attn_norm_rotary_bwd_workspace_bytes(int(d)))
+
+
+def attn_paged_append(K, V, k_cache, v_cache, block_table, lengths, query_starts=None, *, Q=None, rotary=None, norm=None, out=None) -> Optional[torch.Tensor]:
     """Writes the new tokens' K and V rows [T,Hk,d] into the pages of the caches [pages,Hk,page_size,d], and returns the turned Q [T,Hq,d] if Q is given.
 
     block_table int32 [B,table_width]: the pages of each sequence in order.  lengths int32 [B]: its tokens, the new ones included.  query_starts int32 [B+1]: rows
     query_starts[b] .. query_starts[b+1] - 1 are the new tokens of sequence b; None: row b is the one new token of sequence b.  The caches may be views of
-    another order of axes; K and V caches share shape and strides.  rotary: K (and Q, into `out`, which may be Q) are turned by their positions.
+    another order of axes; K and V caches share shape and strides.  rotary: K (and Q, into `out`, which may be Q) are turned by their positions.  norm (a `rotary.HeadNorm`):
+    they are normed before, in the same pass.
     Rows of no sequence are left as they were (unspecified where `out` is made here).  Runs on torch's current stream."""
     if _lib is None:
         load()
-    f, i, m = (None, False, 1.0) if rotary is None else (rotary.frequencies, rotary.interleaved, rotary.magnitude)
+    f, i, m = _rotation(rotary)
+    if norm is not None:
+        return _marshal.paged_norm_append(K, V, k_cache, v_cache, block_table, lengths, query_starts, Q, f, i, m, out, norm.q_weight, norm.k_weight, norm.eps)
     return _marshal.paged_append(K, V, k_cache, v_cache, block_table, lengths, query_starts, Q, f, i, m, out)
 
 

@@ -390,6 +390,8 @@ const char* attn_strerror(int status) {
     case ATTN_ERR_LAUNCH: return "kernel launch failed";
     case ATTN_ERR_PAGES: return "page_size must be a power of two from 16 to 4096; page copies must name pages of the cache, none the destination of one copy and part of another";
     case ATTN_ERR_ROTARY: return "rotary_dim must be even and in [2, d], with frequencies and a finite magnitude (attn_paged_append: Q only with a rotation)";
+    case ATTN_ERR_NORM: return "the norm needs weights aligned to their type and a finite eps > 0";
+    case ATTN_ERR_WINDOW: return "a window needs the causal mask, window >= 1 and sinks >= 0";
     default: return "unknown status";
   }
 }

@@ -35,6 +35,38 @@ struct RotaryCall {
   int64_t position_sb;
 };
 
+// The norm of rows of Q and K (attn_norm_spec, checked).
+struct NormArgs {
+  const void* w[2];     // weights [d] of Q and of K
+  int w_fp32;           // in 32 bits, else in the tensors' type
+  float eps;
+};
+struct NormCall {
+  RotaryCall rotary;    // rotary.rot.r = 0: nothing turns
+  NormArgs norm;
+};
+// One tensor of its backward pass.
+struct NormGrad {
+  const void* x; const void* dy;
+  void* dx;
+  void* dw;             // nullptr: not asked for
+  int H;
+  int64_t xb, xh, xn, gb, gh, gn, yb, yh, yn;
+};
+struct NormBwdCall {
+  NormGrad t[2];
+  int n_tensors;
+  int B, N, d;
+  RotaryArgs rot;       // by the negative angle
+  NormArgs norm;
+  const int* positions;
+  int64_t position_sb;
+  float* partial;       // [workgroups][d]: their shares of the weights' gradients
+};
+// Workgroups of the backward pass at most: eight wavefronts a SIMD.
+constexpr int kNormBlocks = 2048;
+inline size_t norm_workspace_bytes(int d) { return (size_t)kNormBlocks * d * sizeof(float); }
+
 // The sequences of a batch and their pages; see attn_paged_params.
 struct PagedBatch {
   const int* table;
@@ -109,6 +141,9 @@ inline size_t paged_workspace_bytes(int d) {
 
 int launch_rotary(const RotaryCall& c, int dtype, hipStream_t s);
 int launch_append(const AppendCall& c, int dtype, hipStream_t s);
+int launch_norm_rotary(const NormCall& c, int dtype, hipStream_t s);
+int launch_norm_append(const AppendCall& c, const NormArgs& norm, int dtype, hipStream_t s);
+int launch_norm_rotary_bwd(const NormBwdCall& c, int dtype, hipStream_t s);
 int launch_paged_one(const PagedCall& c, int dtype, hipStream_t s);
 int launch_paged_rows(const PagedCall& c, int dtype, hipStream_t s);
 // pairs: host memory, (source, destination) page numbers, checked by the caller; bytes of a row: d * 2.

@@ -10,6 +10,7 @@
 static_assert(sizeof(attn_rotary_spec) == 24 && sizeof(attn_rotary_tensor) == 72 && sizeof(attn_rotary_params) == 72 && sizeof(attn_paged_params) == 176 &&
                   sizeof(attn_paged_copy_params) == 64,
               "the parameter blocks' layout is part of the ABI");
+static_assert(sizeof(attn_norm_spec) == 24 && sizeof(attn_norm_grad) == 112, "the parameter blocks' layout is part of the ABI");
 
 namespace {
 
@@ -45,6 +46,23 @@ int check_rotary(const attn_rotary_spec& r, int d, int inverse, attn::RotaryArgs
   if (r.rotary_dim < 2 || r.rotary_dim > d || r.rotary_dim % 2 != 0) return ATTN_ERR_ROTARY;
   if (r.frequencies == nullptr || !aligned(r.frequencies, 8) || !std::isfinite(r.magnitude)) return ATTN_ERR_ROTARY;
   *out = {r.frequencies, r.rotary_dim, r.interleaved != 0, inverse != 0, r.magnitude};
+  return ATTN_OK;
+}
+
+// a rotation that may be left out
+int check_rotary_or_none(const attn_rotary_spec& r, int d, int inverse, attn::RotaryArgs* out) {
+  if (r.frequencies != nullptr || r.rotary_dim != 0) return check_rotary(r, d, inverse, out);
+  *out = {nullptr, 0, 0, 0, 1.f};
+  return ATTN_OK;
+}
+
+int check_norm(const attn_norm_spec* n, bool with_k, attn::NormArgs* out) {
+  if (n == nullptr) return ATTN_ERR_NULL;
+  if (n->q_weight == nullptr || (with_k && n->k_weight == nullptr)) return ATTN_ERR_NORM;
+  const uintptr_t size = n->weights_fp32 ? 4 : 2;
+  if (!aligned(n->q_weight, size) || (with_k && !aligned(n->k_weight, size))) return ATTN_ERR_NORM;
+  if (!std::isnormal(n->eps) || !(n->eps > 0.f)) return ATTN_ERR_NORM;
+  *out = {{n->q_weight, with_k ? n->k_weight : nullptr}, n->weights_fp32 != 0, n->eps};
   return ATTN_OK;
 }
 
@@ -116,19 +134,21 @@ int check_paged(const attn_paged_params* p, attn::PagedCall* out, attn::PagedSha
   return ATTN_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-int attn_rotary(const attn_rotary_params* p, const attn_rotary_tensor* tensors, int32_t n_tensors) {
-  if (p == nullptr || tensors == nullptr) return ATTN_ERR_NULL;
+int check_rotary_sizes(const attn_rotary_params* p, int32_t n_tensors) {
   if (!dtype_ok(p->dtype)) return ATTN_ERR_DTYPE;
   if (!head_dim_ok(p->d)) return ATTN_ERR_HEADDIM;
   if (p->B <= 0 || p->N <= 0 || (int64_t)p->B * p->N > (int64_t)1 << 28 || n_tensors < 1 || n_tensors > 2) return ATTN_ERR_SHAPE;
   if (p->positions != nullptr && (!aligned(p->positions, 4) || p->position_stride_b < 0 || p->position_stride_b > ((int64_t)1 << 50) / p->B)) return ATTN_ERR_SHAPE;
-  attn::RotaryCall c;
+  return ATTN_OK;
+}
+// Sizes, type, positions and tensors of a rotation (of a norm too: without a rotation if there is none).
+int check_rotary_call(const attn_rotary_params* p, const attn_rotary_tensor* tensors, int32_t n_tensors, bool or_none, attn::RotaryCall* out) {
+  if (p == nullptr || tensors == nullptr) return ATTN_ERR_NULL;
+  int st = check_rotary_sizes(p, n_tensors);
+  if (st != ATTN_OK) return st;
+  attn::RotaryCall& c = *out;
   std::memset(&c, 0, sizeof(c));
-  const int st = check_rotary(p->rotary, p->d, p->inverse, &c.rot);
+  st = or_none ? check_rotary_or_none(p->rotary, p->d, p->inverse, &c.rot) : check_rotary(p->rotary, p->d, p->inverse, &c.rot);
   if (st != ATTN_OK) return st;
   for (int i = 0; i < n_tensors; ++i) {
     const attn_rotary_tensor& t = tensors[i];
@@ -147,19 +167,79 @@ int attn_rotary(const attn_rotary_params* p, const attn_rotary_tensor* tensors, 
   c.B = p->B; c.N = p->N; c.d = p->d;
   c.positions = p->positions;
   c.position_sb = p->position_stride_b;
+  return ATTN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int attn_rotary(const attn_rotary_params* p, const attn_rotary_tensor* tensors, int32_t n_tensors) {
+  attn::RotaryCall c;
+  const int st = check_rotary_call(p, tensors, n_tensors, false, &c);
+  if (st != ATTN_OK) return st;
   return attn::launch_rotary(c, p->dtype, (hipStream_t)p->stream) == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 
-int attn_paged_append(const attn_paged_params* p, const attn_rotary_spec* rotary, const void* K, const void* V, void* k_cache, void* v_cache, const void* Q,
-                      void* Qout) {
-  attn::AppendCall c;
+int attn_norm_rotary(const attn_rotary_params* p, const attn_norm_spec* norm, const attn_rotary_tensor* tensors, int32_t n_tensors) {
+  attn::NormCall c;
+  int st = check_rotary_call(p, tensors, n_tensors, true, &c.rotary);
+  if (st != ATTN_OK) return st;
+  if (p->inverse != 0) return ATTN_ERR_ROTARY;
+  st = check_norm(norm, n_tensors == 2, &c.norm);
+  if (st != ATTN_OK) return st;
+  return attn::launch_norm_rotary(c, p->dtype, (hipStream_t)p->stream) == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
+}
+
+size_t attn_norm_rotary_bwd_workspace_bytes(int32_t d) { return head_dim_ok(d) ? attn::norm_workspace_bytes(d) : 0; }
+
+int attn_norm_rotary_bwd(const attn_rotary_params* p, const attn_norm_spec* norm, const attn_norm_grad* tensors, int32_t n_tensors, void* workspace,
+                         size_t workspace_bytes) {
+  if (p == nullptr || tensors == nullptr) return ATTN_ERR_NULL;
+  int st = check_rotary_sizes(p, n_tensors);
+  if (st != ATTN_OK) return st;
+  attn::NormBwdCall c;
+  std::memset(&c, 0, sizeof(c));
+  st = check_rotary_or_none(p->rotary, p->d, 1, &c.rot);
+  if (st != ATTN_OK) return st;
+  if (p->inverse != 0) return ATTN_ERR_ROTARY;
+  st = check_norm(norm, n_tensors == 2, &c.norm);
+  if (st != ATTN_OK) return st;
+  for (int i = 0; i < n_tensors; ++i) {
+    const attn_norm_grad& t = tensors[i];
+    if (t.H <= 0 || t.H > (1 << 16)) return ATTN_ERR_SHAPE;
+    const Axis xb = {t.x_stride_b, p->B}, xh = {t.x_stride_h, t.H}, xn = {t.x_stride_n, p->N};
+    const Axis gb = {t.dy_stride_b, p->B}, gh = {t.dy_stride_h, t.H}, gn = {t.dy_stride_n, p->N};
+    const Axis yb = {t.dx_stride_b, p->B}, yh = {t.dx_stride_h, t.H}, yn = {t.dx_stride_n, p->N};
+    if (!rows_ok({xb, xh, xn, gb, gh, gn, yb, yh, yn}) || !rows_apart(p->d, yb, yh, yn)) return ATTN_ERR_SHAPE;
+    if (t.x == nullptr || t.dy == nullptr || t.dx == nullptr) return ATTN_ERR_NULL;
+    if (!aligned(t.x, 16) || !aligned(t.dy, 16) || !aligned(t.dx, 16)) return ATTN_ERR_SHAPE;
+    if (!aligned(t.dw, c.norm.w_fp32 ? 4 : 2)) return ATTN_ERR_NORM;
+    c.t[i] = {t.x, t.dy, t.dx, t.dw, t.H, xb.stride, xh.stride, xn.stride, gb.stride, gh.stride, gn.stride, yb.stride, yh.stride, yn.stride};
+  }
+  // (what one thread writes, no other must read or write)
+  for (int i = 0; i < n_tensors; ++i)
+    for (int j = 0; j < n_tensors; ++j)
+      if (c.t[i].dx == c.t[j].x || c.t[i].dx == c.t[j].dy || (i != j && (c.t[i].dx == c.t[j].dx || (c.t[i].dw != nullptr && c.t[i].dw == c.t[j].dw)))) return ATTN_ERR_SHAPE;
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < attn::norm_workspace_bytes(p->d)) return ATTN_ERR_WORKSPACE;
+  c.n_tensors = n_tensors;
+  c.B = p->B; c.N = p->N; c.d = p->d;
+  c.positions = p->positions;
+  c.position_sb = p->position_stride_b;
+  c.partial = (float*)workspace;
+  return attn::launch_norm_rotary_bwd(c, p->dtype, (hipStream_t)p->stream) == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
+}
+
+static int check_append(const attn_paged_params* p, const attn_rotary_spec* rotary, bool normed, const void* K, const void* V, void* k_cache, void* v_cache, const void* Q,
+                        void* Qout, attn::AppendCall* out) {
+  attn::AppendCall& c = *out;
   std::memset(&c, 0, sizeof(c));
   int st = check_batch(p, &c.b);
   if (st != ATTN_OK) return st;
   if (rotary != nullptr) {
     st = check_rotary(*rotary, p->d, 0, &c.rot);
     if (st != ATTN_OK) return st;
-  } else if (Q != nullptr) {
+  } else if (Q != nullptr && !normed) {
     return ATTN_ERR_ROTARY;
   }
   const Axis kt = {p->k_stride_t, p->T}, kh = {p->k_stride_h, p->Hk}, vt = {p->v_stride_t, p->T}, vh = {p->v_stride_h, p->Hk};
@@ -180,7 +260,33 @@ int attn_paged_append(const attn_paged_params* p, const attn_rotary_spec* rotary
   c.d = p->d;
   c.K = K; c.V = V; c.Q = Q; c.Kc = k_cache; c.Vc = v_cache; c.Qo = Qout;
   c.kt = kt.stride; c.kh = kh.stride; c.vt = vt.stride; c.vh = vh.stride;
+  return ATTN_OK;
+}
+
+int attn_paged_append(const attn_paged_params* p, const attn_rotary_spec* rotary, const void* K, const void* V, void* k_cache, void* v_cache, const void* Q,
+                      void* Qout) {
+  attn::AppendCall c;
+  const int st = check_append(p, rotary, false, K, V, k_cache, v_cache, Q, Qout, &c);
+  if (st != ATTN_OK) return st;
   return attn::launch_append(c, p->dtype, (hipStream_t)p->stream) == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
+}
+
+int attn_paged_norm_append(const attn_paged_params* p, const attn_rotary_spec* rotary, const attn_norm_spec* norm, const void* K, const void* V, void* k_cache,
+                           void* v_cache, const void* Q, void* Qout) {
+  attn::AppendCall c;
+  int st = check_append(p, rotary, true, K, V, k_cache, v_cache, Q, Qout, &c);
+  if (st != ATTN_OK) return st;
+  if (rotary == nullptr) c.rot.magnitude = 1.f;
+  attn::NormArgs n;
+  if (norm != nullptr && Q == nullptr) {   // (only K's weights are used then)
+    attn_norm_spec k_only = *norm;
+    k_only.q_weight = norm->k_weight;
+    st = check_norm(&k_only, true, &n);
+  } else {
+    st = check_norm(norm, true, &n);
+  }
+  if (st != ATTN_OK) return st;
+  return attn::launch_norm_append(c, n, p->dtype, (hipStream_t)p->stream) == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 
 size_t attn_paged_workspace_bytes(const attn_paged_params* p) {

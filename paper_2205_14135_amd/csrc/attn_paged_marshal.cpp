@@ -6,6 +6,7 @@
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPGraphsC10Utils.h>
 #include <torch/csrc/autograd/function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/saved_variable.h>
 #include <torch/csrc/autograd/variable.h>
@@ -26,6 +27,13 @@ struct Library {
   decltype(&attn_paged_copy) copy = nullptr;
 };
 Library lib;
+struct NormLibrary {
+  decltype(&attn_norm_rotary) fwd = nullptr;
+  decltype(&attn_norm_rotary_bwd_workspace_bytes) workspace_bytes = nullptr;
+  decltype(&attn_norm_rotary_bwd) bwd = nullptr;
+  decltype(&attn_paged_norm_append) append = nullptr;
+};
+NormLibrary norm_lib;
 
 void expect_args(Py_ssize_t n, Py_ssize_t want) {
   if (n != want || lib.rotary == nullptr) raise(PyExc_TypeError, "internal call with the wrong arguments, or before attach_paged()");
@@ -82,7 +90,7 @@ int32_t narrow(int64_t v) { return v > INT32_MAX ? -1 : (int32_t)v; }   // (the 
 // ---- rotary positions
 
 struct Rotation {
-  at::Tensor frequencies, positions;
+  at::Tensor frequencies, positions;   // frequencies may be undefined where a norm goes without a rotation
   bool interleaved, inverse;
   double magnitude;
 };
@@ -90,6 +98,7 @@ void check_frequencies(const at::Tensor& f) {
   if (f.scalar_type() != at::kDouble || f.dim() != 1 || !f.is_contiguous()) raise(PyExc_TypeError, "frequencies must be a contiguous float64 tensor [rotary_dim / 2]");
 }
 attn_rotary_spec spec_of(const at::Tensor& f, bool interleaved, double magnitude) {
+  if (!f.defined()) return {};
   return {(const double*)f.data_ptr(), narrow(2 * f.size(0)), interleaved, (float)magnitude};
 }
 void check_rotation(const at::Tensor& q, const at::Tensor& k, const Rotation& r) {
@@ -100,7 +109,7 @@ void check_rotation(const at::Tensor& q, const at::Tensor& k, const Rotation& r)
     if (k.scalar_type() != q.scalar_type() || k.size(0) != q.size(0) || k.size(2) != q.size(2) || k.size(3) != q.size(3))
       raise(PyExc_ValueError, "Q and K must share type, batch, length and head dimension");
   }
-  check_frequencies(r.frequencies);
+  if (r.frequencies.defined()) check_frequencies(r.frequencies);
   if (r.positions.defined()) {
     const at::Tensor& p = r.positions;
     const bool one = p.dim() == 1 && p.size(0) == q.size(2), each = p.dim() == 2 && p.size(0) == q.size(0) && p.size(1) == q.size(2);
@@ -109,7 +118,7 @@ void check_rotation(const at::Tensor& q, const at::Tensor& k, const Rotation& r)
   }
   expect_gpu(q, {&k, &r.frequencies, &r.positions});
 }
-int rotate(const at::Tensor& q, const at::Tensor& k, const at::Tensor& qo, const at::Tensor& ko, const Rotation& r) {
+attn_rotary_params params_of(const at::Tensor& q, const Rotation& r) {
   attn_rotary_params p = {};
   p.B = narrow(q.size(0)); p.N = narrow(q.size(2)); p.d = narrow(q.size(3));
   p.dtype = q.scalar_type() == at::kHalf ? ATTN_FP16 : ATTN_BF16;
@@ -120,13 +129,31 @@ int rotate(const at::Tensor& q, const at::Tensor& k, const at::Tensor& qo, const
     p.position_stride_b = r.positions.dim() == 2 ? axis_stride(r.positions, 0) : 0;
   }
   p.stream = current_stream(q);
-  attn_rotary_tensor t[2];
+  return p;
+}
+// the tensors that there are; returns their number
+int fill(attn_rotary_tensor (&t)[2], const at::Tensor& q, const at::Tensor& k, const at::Tensor& qo, const at::Tensor& ko) {
   int n = 0;
   for (const auto& [x, y] : {std::pair<const at::Tensor&, const at::Tensor&>(q, qo), std::pair<const at::Tensor&, const at::Tensor&>(k, ko)}) {
     if (!x.defined()) continue;
     t[n++] = {x.data_ptr(), y.data_ptr(), narrow(x.size(1)), axis_stride(x, 0), axis_stride(x, 1), axis_stride(x, 2), axis_stride(y, 0), axis_stride(y, 1), axis_stride(y, 2)};
   }
+  return n;
+}
+int rotate(const at::Tensor& q, const at::Tensor& k, const at::Tensor& qo, const at::Tensor& ko, const Rotation& r) {
+  const attn_rotary_params p = params_of(q, r);
+  attn_rotary_tensor t[2];
+  const int n = fill(t, q, k, qo, ko);
   return lib.rotary(&p, t, n);
+}
+// outputs that the caller gives for Q and K
+void check_outputs(const at::Tensor& q, const at::Tensor& k, const at::Tensor& qo, const at::Tensor& ko) {
+  for (const auto& [x, y] : {std::pair<const at::Tensor&, const at::Tensor&>(q, qo), std::pair<const at::Tensor&, const at::Tensor&>(k, ko)}) {
+    if (!y.defined()) continue;
+    if (!x.defined()) raise(PyExc_ValueError, "an output for K without K");
+    expect_like(y, x, "an output");
+    expect_rows(y, 4, "expected a [B,H,N,d] tensor with contiguous last axis");
+  }
 }
 
 // rotary(Q, K, frequencies, interleaved, magnitude, positions, inverse, Qout, Kout) -> (Q', K')
@@ -136,12 +163,7 @@ PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor &q = tensor(a[0]), k = maybe(a[1]);
     const Rotation r = {tensor(a[2]), maybe(a[5]), truth(a[3]), truth(a[6]), number(a[4])};
     at::Tensor qo = maybe(a[7]), ko = maybe(a[8]);
-    for (const auto& [x, y] : {std::pair<const at::Tensor&, const at::Tensor&>(q, qo), std::pair<const at::Tensor&, const at::Tensor&>(k, ko)}) {
-      if (!y.defined()) continue;
-      if (!x.defined()) raise(PyExc_ValueError, "an output for K without K");
-      expect_like(y, x, "an output");
-      expect_rows(y, 4, "expected a [B,H,N,d] tensor with contiguous last axis");
-    }
+    check_outputs(q, k, qo, ko);
     check_rotation(q, k, r);
     expect_gpu(q, {&qo, &ko});
     const c10::DeviceGuard guard(q.device());
@@ -277,6 +299,196 @@ PyObject* py_rotary_embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- the norm of Q and K, with the rotation
+
+struct Norm { at::Tensor wq, wk; double eps; };   // wk may be undefined where there is no K
+void check_norm(const at::Tensor& q, const at::Tensor& k, const Norm& n) {
+  for (const at::Tensor* w : {&n.wq, &n.wk}) {
+    if (!w->defined()) continue;
+    if (w->dim() != 1 || w->size(0) != q.size(q.dim() - 1) || !w->is_contiguous()) raise(PyExc_ValueError, "the norm's weights must be contiguous tensors [d]");
+    if ((w->scalar_type() != at::kFloat && w->scalar_type() != q.scalar_type()) || (n.wq.defined() && w->scalar_type() != n.wq.scalar_type()))
+      raise(PyExc_TypeError, "the norm's weights must be float32 or of the tensors' type, both the same");
+  }
+  if (!n.wq.defined() || (k.defined() && !n.wk.defined())) raise(PyExc_ValueError, "the norm has no weights for a tensor that is given");
+  expect_gpu(q, {&n.wq, &n.wk});
+}
+attn_norm_spec norm_spec(const Norm& n) {
+  const at::Tensor& w = n.wq.defined() ? n.wq : n.wk;
+  return {ptr(n.wq), ptr(n.wk), w.scalar_type() == at::kFloat, (float)n.eps};
+}
+int norm_rotate(const at::Tensor& q, const at::Tensor& k, const at::Tensor& qo, const at::Tensor& ko, const Norm& n, const Rotation& r) {
+  const attn_rotary_params p = params_of(q, r);
+  const attn_norm_spec s = norm_spec(n);
+  attn_rotary_tensor t[2];
+  const int count = fill(t, q, k, qo, ko);
+  return norm_lib.fwd(&p, &s, t, count);
+}
+// What a backward call reads and writes for one tensor; dw may be undefined.
+struct Grad { at::Tensor x, dy, dx, w, dw; };
+// (of one or two tensors; the first weights are the first tensor's)
+int norm_gradients(const std::vector<Grad>& g, double eps, const Rotation& r, const at::Tensor& ws) {
+  const attn_rotary_params p = params_of(g[0].x, r);
+  attn_norm_grad t[2] = {};
+  for (size_t i = 0; i < g.size(); ++i) {
+    const at::Tensor &x = g[i].x, &y = g[i].dy, &d = g[i].dx;
+    t[i] = {x.data_ptr(), y.data_ptr(), d.data_ptr(), const_cast<void*>(ptr(g[i].dw)), narrow(x.size(1)), axis_stride(x, 0), axis_stride(x, 1), axis_stride(x, 2),
+            axis_stride(y, 0), axis_stride(y, 1), axis_stride(y, 2), axis_stride(d, 0), axis_stride(d, 1), axis_stride(d, 2)};
+  }
+  const attn_norm_spec s = {ptr(g[0].w), g.size() > 1 ? ptr(g[1].w) : nullptr, g[0].w.scalar_type() == at::kFloat, (float)eps};
+  return norm_lib.bwd(&p, &s, t, (int)g.size(), ws.data_ptr(), (size_t)ws.numel() * ws.element_size());
+}
+at::Tensor norm_workspace(const at::Tensor& x) {
+  return at::empty({(int64_t)std::max<size_t>(norm_lib.workspace_bytes(narrow(x.size(3))), 256)}, x.options().dtype(at::kByte));
+}
+void check_no_lost_positions(const Rotation& r) {
+  if (r.positions.defined() && !r.frequencies.defined()) raise(PyExc_ValueError, "positions are of no use without rotary");
+}
+
+// norm_rotary(Q, K, q_weight, k_weight, eps, frequencies, interleaved, magnitude, positions, Qout, Kout) -> (Q', K')
+PyObject* py_norm_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expect_args(n, 11);
+    const at::Tensor &q = tensor(a[0]), k = maybe(a[1]);
+    const Norm norm = {maybe(a[2]), maybe(a[3]), number(a[4])};
+    const Rotation r = {maybe(a[5]), maybe(a[8]), truth(a[6]), false, number(a[7])};
+    at::Tensor qo = maybe(a[9]), ko = maybe(a[10]);
+    check_outputs(q, k, qo, ko);
+    check_rotation(q, k, r);
+    check_no_lost_positions(r);
+    check_norm(q, k, norm);
+    expect_gpu(q, {&qo, &ko});
+    const c10::DeviceGuard guard(q.device());
+    if (!qo.defined()) qo = output_like(q);
+    if (k.defined() && !ko.defined()) ko = output_like(k);
+    check_status(without_gil([&] { return norm_rotate(q, k, qo, ko, norm, r); }), "attn_norm_rotary");
+    PyObject* const second = k.defined() ? (a[10] != Py_None ? Py_NewRef(a[10]) : wrap(ko)) : Py_NewRef(Py_None);
+    return tuple({a[9] != Py_None ? Py_NewRef(a[9]) : wrap(qo), second});
+  });
+}
+
+// norm_rotary_bwd(Q, K, dQ', dK', q_weight, k_weight, eps, frequencies, interleaved, magnitude, positions, workspace) -> (dQ, dK, dq_weight, dk_weight)
+PyObject* py_norm_rotary_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expect_args(n, 12);
+    const at::Tensor &q = tensor(a[0]), k = maybe(a[1]), &gq = tensor(a[2]), gk = maybe(a[3]);
+    const Norm norm = {maybe(a[4]), maybe(a[5]), number(a[6])};
+    const Rotation r = {maybe(a[7]), maybe(a[10]), truth(a[8]), false, number(a[9])};
+    at::Tensor ws = maybe(a[11]);
+    if (k.defined() != gk.defined()) raise(PyExc_ValueError, "K and its gradient go together");
+    check_outputs(q, k, gq, gk);
+    check_rotation(q, k, r);
+    check_no_lost_positions(r);
+    check_norm(q, k, norm);
+    if (ws.defined() && !ws.is_contiguous()) raise(PyExc_ValueError, "the workspace must be contiguous");
+    expect_gpu(q, {&gq, &gk, &ws});
+    const c10::DeviceGuard guard(q.device());
+    if (!ws.defined()) ws = norm_workspace(q);
+    std::vector<Grad> g = {{q, gq, packed_like(q), norm.wq, at::empty_like(norm.wq)}};
+    if (k.defined()) g.push_back({k, gk, packed_like(k), norm.wk, at::empty_like(norm.wk)});
+    check_status(without_gil([&] { return norm_gradients(g, norm.eps, r, ws); }), "attn_norm_rotary_bwd");
+    if (!k.defined()) return tuple({wrap(g[0].dx), Py_NewRef(Py_None), wrap(g[0].dw), Py_NewRef(Py_None)});
+    return tuple({wrap(g[0].dx), wrap(g[1].dx), wrap(g[0].dw), wrap(g[1].dw)});
+  });
+}
+
+struct NormRotaryBackward : torch::autograd::Node {
+  SavedVariable x[2], w[2], frequencies, positions;
+  bool interleaved = false;
+  double magnitude = 1.0, eps = 0.0;
+  int64_t pairs = 0;
+
+  // inputs: q, k, q_weight, k_weight
+  variable_list apply(variable_list&& grads) override {
+    Rotation r = {at::Tensor(), at::Tensor(), interleaved, false, magnitude};
+    at::Tensor xs[2], ws[2];
+    {
+      const std::lock_guard<std::mutex> lock(mutex_);
+      r.frequencies = frequencies.unpack();
+      r.positions = positions.unpack();
+      for (int i = 0; i < 2; ++i) {
+        xs[i] = x[i].unpack();
+        ws[i] = w[i].unpack();
+      }
+    }
+    variable_list out(4);
+    std::vector<Grad> g;
+    int which[2];
+    for (int i = 0; i < 2; ++i) {
+      if (!grads[i].defined() || !(should_compute_output(i) || should_compute_output(2 + i))) continue;
+      // (hooks of the program may have handed back something else than what was saved)
+      const at::Tensor &f = r.frequencies, &p = r.positions;
+      const bool ok = xs[i].defined() && xs[i].dim() == 4 && xs[i].sizes() == grads[i].sizes() && xs[i].scalar_type() == grads[i].scalar_type() && xs[i].device() == grads[i].device() &&
+                      ws[i].defined() && ws[i].dim() == 1 && ws[i].size(0) == xs[i].size(3) && ws[i].is_contiguous() && ws[i].device() == xs[i].device() &&
+                      (ws[i].scalar_type() == at::kFloat || ws[i].scalar_type() == xs[i].scalar_type()) && (g.empty() || ws[i].scalar_type() == g[0].w.scalar_type()) &&
+                      (pairs == 0 ? !f.defined() : f.defined() && f.scalar_type() == at::kDouble && f.dim() == 1 && f.size(0) == pairs && f.is_contiguous() && f.device() == xs[i].device()) &&
+                      (!p.defined() || (p.device() == xs[i].device() && p.scalar_type() == at::kInt &&
+                                        (p.dim() == 1 ? p.size(0) == xs[i].size(2) : p.dim() == 2 && p.size(0) == xs[i].size(0) && p.size(1) == xs[i].size(2)) &&
+                                        (xs[i].size(2) <= 1 || p.stride(p.dim() - 1) == 1)));
+      if (!ok) refused_in_backward([] { raise(PyExc_ValueError, "the saved tensors are not those of the forward call"); });
+      const c10::DeviceGuard guard(xs[i].device());
+      const at::Tensor from = readable(xs[i]);
+      which[g.size()] = i;
+      g.push_back({from, readable(grads[i]), packed_like(xs[i]), ws[i], should_compute_output(2 + i) ? at::empty_like(ws[i]) : at::Tensor()});
+    }
+    if (g.empty()) return out;
+    const c10::DeviceGuard guard(g[0].x.device());
+    const int status = norm_gradients(g, eps, r, norm_workspace(g[0].x));
+    if (status != ATTN_OK) refused_in_backward([&] { check_status(status, "attn_norm_rotary_bwd"); });
+    for (size_t n = 0; n < g.size(); ++n) {
+      if (should_compute_output(which[n])) out[which[n]] = g[n].dx;
+      out[2 + which[n]] = g[n].dw;
+    }
+    if (at::GradMode::is_enabled()) {   // the gradients have no gradients: to differentiate them again is an error, whichever of the inputs is asked for
+      torch::autograd::edge_list edges = next_edges();
+      const std::shared_ptr<torch::autograd::Node> error(
+          new torch::autograd::Error("the gradients of norm_rotary_embedding cannot be differentiated again", std::move(edges)), torch::autograd::deleteNode);
+      for (at::Tensor& t : out)
+        if (t.defined()) torch::autograd::set_history(t, error);
+    }
+    return out;
+  }
+  void release_variables() override {
+    const std::lock_guard<std::mutex> lock(mutex_);
+    for (SavedVariable* s : {&x[0], &x[1], &w[0], &w[1], &frequencies, &positions}) s->reset_data();
+  }
+  std::string name() const override { return "NormRotaryBackward"; }
+};
+
+// norm_rotary_embedding(Q, K, q_weight, k_weight, eps, frequencies, interleaved, magnitude, positions, V) -> (Q', K'), differentiable.  V: of the same pass, or None.
+PyObject* py_norm_rotary_embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expect_args(n, 10);
+    const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), v = maybe(a[9]);
+    const Norm norm = {maybe(a[2]), maybe(a[3]), number(a[4])};
+    const Rotation r = {maybe(a[5]), maybe(a[8]), truth(a[6]), false, number(a[7])};
+    check_rotation(q, k, r);
+    check_no_lost_positions(r);
+    check_norm(q, k, norm);
+    const c10::DeviceGuard guard(q.device());
+    const bool track = torch::autograd::compute_requires_grad(q, k, norm.wq, norm.wk);
+    if (at::GradMode::is_enabled()) refuse_eager_graphs({&q, &k, &v, &norm.wq, &norm.wk});
+    at::Tensor qo = output_like(q), ko = output_like(k);
+    check_status(without_gil([&] { return norm_rotate(q, k, qo, ko, norm, r); }), "attn_norm_rotary");
+    if (track) {
+      const std::shared_ptr<NormRotaryBackward> node(new NormRotaryBackward(), torch::autograd::deleteNode);
+      node->set_next_edges(torch::autograd::collect_next_edges(q, k, norm.wq, norm.wk));
+      node->x[0] = SavedVariable(q, false);
+      node->x[1] = SavedVariable(k, false);
+      node->w[0] = SavedVariable(norm.wq, false);
+      node->w[1] = SavedVariable(norm.wk, false);
+      node->frequencies = SavedVariable(r.frequencies, false);
+      node->positions = SavedVariable(r.positions, false);
+      node->pairs = r.frequencies.defined() ? r.frequencies.size(0) : 0;
+      node->interleaved = r.interleaved;
+      node->magnitude = r.magnitude;
+      node->eps = norm.eps;
+      torch::autograd::set_history(qo, node);
+      torch::autograd::set_history(ko, node);
+    }
+    return tuple({wrap(qo), wrap(ko)});
+  });
+}
+
 // ---- the paged cache
 
 // What the calls share: caches, table, lengths, starts.
@@ -319,10 +531,10 @@ void expect_gpu(const at::Tensor& rows, const Batch& b, std::initializer_list<co
   expect_gpu(rows, others);
 }
 
-// paged_append(K, V, k_cache, v_cache, block_table, lengths, query_starts, Q, frequencies, interleaved, magnitude, out) -> the turned Q, or None
-PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+// paged_append(K, V, k_cache, v_cache, block_table, lengths, query_starts, Q, frequencies, interleaved, magnitude, out[, q_weight, k_weight, eps]) -> the turned Q, or None
+PyObject* append(PyObject* const* a, Py_ssize_t n, bool normed) {
   return guarded([&]() -> PyObject* {
-    expect_args(n, 12);
+    expect_args(n, normed ? 15 : 12);
     const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]);
     const Batch b = batch_of(a + 2);
     attn_paged_params p = params_of(k, b);
@@ -339,7 +551,7 @@ PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       spec = spec_of(f, truth(a[9]), number(a[10]));
     }
     if (q.defined()) {
-      if (!f.defined()) raise(PyExc_ValueError, "Q is taken only with a rotation");
+      if (!f.defined() && !normed) raise(PyExc_ValueError, "Q is taken only with a rotation");
       expect_rows(q, 3, "expected a [T,heads,d] tensor with contiguous last axis");
       if (q.scalar_type() != k.scalar_type() || q.size(0) != k.size(0) || q.size(2) != k.size(2)) raise(PyExc_ValueError, "Q and K must share type, tokens and head dimension");
       if (out.defined()) {
@@ -350,6 +562,15 @@ PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       raise(PyExc_ValueError, "an output for Q without Q");
     }
     expect_gpu(k, b, {&v, &q, &f, &out});
+    attn_norm_spec norm = {};
+    Norm weights = {};
+    if (normed) {
+      weights = {maybe(a[12]), maybe(a[13]), number(a[14])};
+      if (!weights.wk.defined()) raise(PyExc_ValueError, "the norm has no weights for a tensor that is given");
+      if (!q.defined()) weights.wq = weights.wk;   // (of no use then)
+      check_norm(k, k, weights);
+      norm = norm_spec(weights);
+    }
     const c10::DeviceGuard guard(k.device());
     p.stream = current_stream(k);
     if (q.defined()) {
@@ -358,11 +579,16 @@ PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       p.q_stride_t = axis_stride(q, 0); p.q_stride_h = axis_stride(q, 1); p.o_stride_t = axis_stride(out, 0); p.o_stride_h = axis_stride(out, 1);
     }
     check_status(without_gil([&] {
-      return lib.append(&p, f.defined() ? &spec : nullptr, k.data_ptr(), v.data_ptr(), b.kc.data_ptr(), b.vc.data_ptr(), ptr(q), const_cast<void*>(ptr(out)));
-    }), "attn_paged_append");
+      const attn_rotary_spec* const turn = f.defined() ? &spec : nullptr;
+      void* const qo = const_cast<void*>(ptr(out));
+      return normed ? norm_lib.append(&p, turn, &norm, k.data_ptr(), v.data_ptr(), b.kc.data_ptr(), b.vc.data_ptr(), ptr(q), qo)
+                    : lib.append(&p, turn, k.data_ptr(), v.data_ptr(), b.kc.data_ptr(), b.vc.data_ptr(), ptr(q), qo);
+    }), normed ? "attn_paged_norm_append" : "attn_paged_append");
     return !q.defined() ? Py_NewRef(Py_None) : (a[11] != Py_None ? Py_NewRef(a[11]) : wrap(out));
   });
 }
+PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return append(a, n, false); }
+PyObject* py_norm_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return append(a, n, true); }
 
 // paged_fwd(Q, k_cache, v_cache, block_table, lengths, query_starts, softmax_scale, causal, out, lse, workspace) -> (O, LSE)
 PyObject* py_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -458,9 +684,28 @@ PyObject* py_attach(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// attach_norm(addresses of attn_norm_rotary, attn_norm_rotary_bwd_workspace_bytes, attn_norm_rotary_bwd, attn_paged_norm_append)
+PyObject* py_attach_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 4) raise(PyExc_TypeError, "attach_norm() takes four addresses");
+    NormLibrary l;
+    l.fwd = (decltype(l.fwd))low64(a[0]);
+    l.workspace_bytes = (decltype(l.workspace_bytes))low64(a[1]);
+    l.bwd = (decltype(l.bwd))low64(a[2]);
+    l.append = (decltype(l.append))low64(a[3]);
+    norm_lib = l;
+    Py_RETURN_NONE;
+  });
+}
+
 }  // namespace
 
 PyMethodDef marshal::paged_methods[] = {
+    {"attach_norm", (PyCFunction)(void*)py_attach_norm, METH_FASTCALL, nullptr},
+    {"norm_rotary", (PyCFunction)(void*)py_norm_rotary, METH_FASTCALL, nullptr},
+    {"norm_rotary_bwd", (PyCFunction)(void*)py_norm_rotary_bwd, METH_FASTCALL, nullptr},
+    {"norm_rotary_embedding", (PyCFunction)(void*)py_norm_rotary_embedding, METH_FASTCALL, nullptr},
+    {"paged_norm_append", (PyCFunction)(void*)py_norm_append, METH_FASTCALL, nullptr},
     {"attach_paged", (PyCFunction)(void*)py_attach, METH_FASTCALL, nullptr},
     {"rotary", (PyCFunction)(void*)py_rotary, METH_FASTCALL, nullptr},
     {"rotary_embedding", (PyCFunction)(void*)py_rotary_embedding, METH_FASTCALL, nullptr},

@@ -3,6 +3,7 @@
 Pair i of the first r columns, columns (2 i, 2 i + 1) or (i, i + r / 2), at position p turns by p * frequencies[i] and is multiplied by
 `magnitude`; columns behind r stay as they are.  A product of a turned query and a turned key then depends on the difference of their positions.
 `Rotary` is what `autograd.rotary_embedding`, `autograd.flash_attention`, `binding.attn_rotary` and `binding.attn_paged_append` take.
+`HeadNorm` is the norm of every row of Q and K that models put in front of the rotation.
 """
 from __future__ import annotations
 
@@ -65,3 +66,27 @@ class Rotary:
         """From `rotary_frequencies` (its `scaling`, `factor`, ...)."""
         frequencies, magnitude = rotary_frequencies(rotary_dim, base, **scaling)
         return cls(frequencies.to(device), interleaved=interleaved, magnitude=magnitude)
+
+
+class HeadNorm:
+    """The norm of every row of Q and of K: weight * x / sqrt(mean(x^2) + eps), one weight [d] for all heads of a tensor.
+
+    Weights: contiguous [d], float32 or of the tensors' type, both the same, on the GPU of the tensors (parameters of a module: they get gradients
+    through `autograd.norm_rotary_embedding`).  k_weight may be left out where there is no K.  `autograd.norm_rotary_embedding`, `autograd.flash_attention`,
+    `binding.attn_norm_rotary` and `binding.attn_paged_append` take it."""
+
+    __slots__ = ("q_weight", "k_weight", "eps")
+
+    def __init__(self, q_weight: torch.Tensor, k_weight: Optional[torch.Tensor] = None, *, eps: float = 1e-6):
+        for w in (q_weight, k_weight):
+            if w is None:
+                continue
+            if w.dim() != 1 or not w.is_contiguous() or w.numel() == 0:
+                raise ValueError("the norm's weights must be contiguous tensors [d]")
+            if w.dtype not in (torch.float32, torch.float16, torch.bfloat16) or w.dtype != q_weight.dtype:
+                raise TypeError("the norm's weights must be float32 or of the tensors' type, both the same")
+        if k_weight is not None and k_weight.shape != q_weight.shape:
+            raise ValueError("the norm's weights must have the same length")
+        if not (math.isfinite(eps) and 1e-37 <= eps <= 1e37):
+            raise ValueError("eps must be finite and positive, and a float32 that is not subnormal")
+        self.q_weight, self.k_weight, self.eps = q_weight, k_weight, float(eps)
