@@ -212,6 +212,20 @@ int attn_blocksparse_bwd(const attn_params* p, const uint8_t* block_mask, int32_
                          void* dQ, void* dK, void* dV, void* workspace, size_t workspace_bytes);
 
 /*
+ * Attention with a sliding window and first tokens that stay visible: as attn_fwd with the causal mask (p->causal must be set), but key j is visible to query i iff
+ * j <= i and (i - j < window or j < sinks): a query sees the last `window` keys, its own among them, and the first `sinks` of its sequence.  window >= 1, sinks >= 0.
+ * The work is linear in N (window + sinks).  Where nothing is hidden (window + sinks >= N) this is attn_fwd.
+ */
+int attn_window_fwd(const attn_params* p, int32_t window, int32_t sinks, const void* Q, const void* K, const void* V, void* O, float* LSE);
+
+/* Bytes of scratch for attn_window_bwd: what attn_bwd needs, and pieces of dK and dV in float32 for the keys that are sinks (32 at a time).  0 if the params are invalid. */
+size_t attn_window_bwd_workspace_bytes(const attn_params* p, int32_t window, int32_t sinks);
+
+/* Its backward pass: arguments as attn_bwd, O and LSE from attn_window_fwd.  Gradients are the same bits in every call. */
+int attn_window_bwd(const attn_params* p, int32_t window, int32_t sinks, const void* Q, const void* K, const void* V, const void* O, const void* dO, const float* LSE,
+                    void* dQ, void* dK, void* dV, void* workspace, size_t workspace_bytes);
+
+/*
  * Profiling aid for the backward pass (Algorithm 4 as attn_bwd / attn_blocksparse_bwd run it):
  * identical to attn_bwd when block_mask is NULL and to attn_blocksparse_bwd otherwise, and in
  * addition records the caller's four hipEvent_t handles on p->stream: events[0] and events[1]

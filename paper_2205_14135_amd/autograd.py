@@ -46,6 +46,22 @@ class _FlashAttention(torch.autograd.Function):
         return dq, dk, dv, None, None, None, None, None, None, None
 
 
+class _WindowAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, softmax_scale, dropout_p, seed, offset, key_lengths, window, sinks):
+        ctx.kw = dict(softmax_scale=softmax_scale, dropout_p=dropout_p, seed=seed, offset=offset, key_lengths=key_lengths, window=window, sinks=sinks)
+        out, lse = binding.attn_window_fwd(q, k, v, **ctx.kw)
+        ctx.save_for_backward(q, k, v, out, lse)
+        return out
+
+    @staticmethod
+    def backward(ctx, d_out):
+        q, k, v, out, lse = ctx.saved_tensors
+        if d_out.shape != q.shape or d_out.stride() != q.stride():
+            d_out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=q.device).copy_(d_out)
+        return (*binding.attn_window_bwd(q, k, v, out, d_out, lse, **ctx.kw), *(None,) * 7)
+
+
 class _RotaryEmbedding(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, frequencies, interleaved, magnitude, positions, inverse):
@@ -136,7 +152,8 @@ def flash_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, softma
                     causal: bool = False, dropout_p: float = 0.0, seed: Optional[int] = None, offset: int = 0,
                     key_lengths: Optional[torch.Tensor] = None,
                     block_mask: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
-                    positions: Optional[torch.Tensor] = None, norm: Optional[HeadNorm] = None) -> torch.Tensor:
+                    positions: Optional[torch.Tensor] = None, norm: Optional[HeadNorm] = None,
+                    window: Optional[int] = None, sinks: int = 0) -> torch.Tensor:
     """softmax(scale * q k^T + mask) v with dropout on the probabilities; exact attention.
 
     q, k, v: [B,H,N,d] fp16 or bf16 CUDA tensors with identical shape and strides, d contiguous,
@@ -145,7 +162,18 @@ def flash_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, softma
     With dropout_p > 0 the mask is a pure function of (seed, offset, b, h, i, j); seed defaults to a
     draw from torch's CPU generator, so torch.manual_seed makes a run reproducible.  With `rotary`, q and k are
     turned by their `positions` first (`rotary_embedding`), with `norm` their rows are normed before that, in the same pass (`norm_rotary_embedding`).
+    With `window` (causal only, without a block mask) a query sees the last `window` keys, its own among them, and the first `sinks` keys of its sequence; the work grows with
+    N (window + sinks).  In a captured graph that holds the backward pass too, such a call asks of its leaves what `rotary_embedding` does.
     """
+    if window is not None:
+        if not causal:
+            raise ValueError("a window needs the causal mask")
+        if block_mask is not None:
+            raise ValueError("a window and a block mask do not go together")
+        if window < 1 or sinks < 0:
+            raise ValueError("window must be at least 1, and sinks must not be negative")
+    elif sinks != 0:
+        raise ValueError("sinks are of no use without a window")
     if not (q.is_cuda and k.is_cuda and v.is_cuda):
         raise RuntimeError("flash_attention runs on the GPU only: there is no CPU path")
     if softmax_scale is None:
@@ -160,6 +188,10 @@ def flash_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, softma
         q, k = _turned(q, k, v, rotary, positions)
     elif positions is not None:
         raise ValueError("positions are of no use without rotary")
+    if window is not None:
+        if _node_in_python():
+            return _WindowAttention.apply(q, k, v, float(softmax_scale), float(dropout_p), int(seed or 0), int(offset), key_lengths, window, sinks)
+        return binding._marshal.attention(q, k, v, float(softmax_scale), True, float(dropout_p), int(seed or 0), int(offset), key_lengths, None, window, sinks)
     if _node_in_python():
         apply = _FlashAttention.apply
     else:

@@ -25,6 +25,7 @@ SYMBOLS = (
     "attn_blocksparse_bwd", "attn_bwd_timed", "attn_debug_dropout_mask", "attn_debug_mfma_rate", "attn_debug_kernel_choice", "attn_debug_bwd_kernel", "attn_debug_set_variant", "attn_strerror",
     "attn_version", "attn_rotary", "attn_paged_append", "attn_paged_workspace_bytes", "attn_paged_fwd", "attn_paged_copy",
     "attn_norm_rotary", "attn_norm_rotary_bwd_workspace_bytes", "attn_norm_rotary_bwd", "attn_paged_norm_append",
+    "attn_window_fwd", "attn_window_bwd_workspace_bytes", "attn_window_bwd",
 )
 
 
@@ -106,6 +107,11 @@ def _attach(lib: ctypes.CDLL) -> None:
         "attn_blocksparse_bwd_workspace_bytes")))
 
 
+def _attach_window(lib: ctypes.CDLL) -> None:
+    """The same for attention with a sliding window."""
+    _marshal.attach_window(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in ("attn_window_fwd", "attn_window_bwd", "attn_window_bwd_workspace_bytes")))
+
+
 def _attach_paged(lib: ctypes.CDLL) -> None:
     """The same for the rotary positions and the paged cache."""
     _marshal.attach_paged(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
@@ -140,6 +146,12 @@ def load() -> ctypes.CDLL:
     lib.attn_blocksparse_fwd.restype = ctypes.c_int
     lib.attn_blocksparse_bwd.argtypes = [P, vp, i32, i64] + [vp] * 9 + [vp, sz]
     lib.attn_blocksparse_bwd.restype = ctypes.c_int
+    lib.attn_window_fwd.argtypes = [P, i32, i32, vp, vp, vp, vp, vp]
+    lib.attn_window_fwd.restype = ctypes.c_int
+    lib.attn_window_bwd_workspace_bytes.argtypes = [P, i32, i32]
+    lib.attn_window_bwd_workspace_bytes.restype = sz
+    lib.attn_window_bwd.argtypes = [P, i32, i32] + [vp] * 9 + [vp, sz]
+    lib.attn_window_bwd.restype = ctypes.c_int
     lib.attn_bwd_timed.argtypes = [P, vp, i32, i64] + [vp] * 9 + [vp, sz, ctypes.POINTER(vp)]
     lib.attn_bwd_timed.restype = ctypes.c_int
     lib.attn_debug_dropout_mask.argtypes = [P, vp]
@@ -175,6 +187,7 @@ def load() -> ctypes.CDLL:
     lib.attn_version.argtypes = []
     lib.attn_version.restype = ctypes.c_int
     _attach(lib)
+    _attach_window(lib)
     _attach_paged(lib)
     _lib = lib
     return lib
@@ -312,6 +325,27 @@ def attn_blocksparse_bwd(Q, K, V, O, dO, LSE, block_mask, *, softmax_scale, mask
     dQ, dK, dV = (None, None, None) if grads is None else grads
     return _marshal.blocksparse_bwd(Q, K, V, O, dO, LSE, softmax_scale, causal, dropout_p, seed, offset, o_fp32, stream,
                                     key_lengths, workspace, grads is None, dQ, dK, dV, block_mask, mask_block)
+
+
+def attn_window_fwd(Q, K, V, *, window, sinks=0, softmax_scale, dropout_p=0.0, seed=0, offset=0, o_fp32=False, out=None, lse=None, stream=None, key_lengths=None):
+    """attn_fwd under the causal mask in which a query sees the last `window` keys, its own among them, and the first `sinks` keys of its sequence."""
+    if _lib is None:
+        load()
+    return _marshal.window_fwd(Q, K, V, softmax_scale, True, dropout_p, seed, offset, o_fp32, stream, key_lengths, out, lse, window, sinks)
+
+
+def attn_window_bwd_workspace_bytes(p: AttnParams, window: int, sinks: int = 0) -> int:
+    return int(load().attn_window_bwd_workspace_bytes(ctypes.byref(p), int(window), int(sinks)))
+
+
+def attn_window_bwd(Q, K, V, O, dO, LSE, *, window, sinks=0, softmax_scale, dropout_p=0.0, seed=0, offset=0, o_fp32=False, workspace=None, grads=None, stream=None,
+                    key_lengths=None):
+    """dQ, dK, dV of attn_window_fwd (O, LSE from it with the same options)."""
+    if _lib is None:
+        load()
+    dQ, dK, dV = (None, None, None) if grads is None else grads
+    return _marshal.window_bwd(Q, K, V, O, dO, LSE, softmax_scale, True, dropout_p, seed, offset, o_fp32, stream, key_lengths, workspace, grads is None, dQ, dK, dV,
+                               window, sinks)
 
 
 def attn_bwd_timed(Q, K, V, O, dO, LSE, events, *, softmax_scale, block_mask=None, mask_block=128,

@@ -1,6 +1,7 @@
 // C-ABI front end: argument checks (host only, before any launch) and kernel dispatch.
 #include "../../include/attn.h"
 #include "attn_common.h"
+#include "attn_window.h"
 
 #include <algorithm>
 #include <atomic>
@@ -190,6 +191,20 @@ int bwd_common(const attn_params* p, const uint8_t* mask, int64_t mask_sh, bool 
   return e == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 
+// attn_window_fwd / _bwd: the checked params and the window, cut to the problem's length.
+int check_window(const attn_params* p, int32_t window, int32_t sinks, Checked* c, attn::WindowArgs* out) {
+  const int st = check_params(p, c);
+  if (st != ATTN_OK) return st;
+  if (p->causal == 0 || window < 1 || sinks < 0) return ATTN_ERR_WINDOW;
+  attn::WindowArgs& w = *out;
+  std::memset(&w, 0, sizeof(w));
+  w.k = c->k;
+  w.window = std::min(window, p->N);
+  w.sinks = std::min(sinks, p->N);
+  if (attn::window_hides(p->N, w.window, w.sinks)) attn::window_plan(w, p->d);
+  return ATTN_OK;
+}
+
 // Device address of the current GPU's copy of `scratch`: looked up once per device, with that
 // device current, and kept; nullptr if the runtime cannot tell.  Allocates nothing.
 void* static_scratch() {
@@ -306,6 +321,46 @@ int attn_blocksparse_bwd(const attn_params* p, const uint8_t* block_mask, int32_
   if (st != ATTN_OK) return st;
   return bwd_common(p, block_mask, mask_stride_h, true, Q, K, V, O, dO, LSE, dQ, dK, dV, workspace,
                     workspace_bytes);
+}
+
+int attn_window_fwd(const attn_params* p, int32_t window, int32_t sinks, const void* Q, const void* K, const void* V, void* O, float* LSE) {
+  Checked c;
+  attn::WindowArgs w;
+  const int st = check_window(p, window, sinks, &c, &w);
+  if (st != ATTN_OK) return st;
+  if (!attn::window_hides(p->N, w.window, w.sinks)) return fwd_common(p, nullptr, 0, false, Q, K, V, O, LSE);
+  if (!Q || !K || !V || !O || !LSE) return ATTN_ERR_NULL;
+  if (!aligned16({Q, K, V, O}) || ((uintptr_t)LSE & 3u) != 0) return ATTN_ERR_SHAPE;
+  w.k.Q = Q; w.k.K = K; w.k.V = V; w.k.O = O; w.k.LSE = LSE;
+  return attn::launch_window_fwd(w, c.dtype, c.d, c.dropout, c.stream) == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
+}
+
+size_t attn_window_bwd_workspace_bytes(const attn_params* p, int32_t window, int32_t sinks) {
+  Checked c;
+  attn::WindowArgs w;
+  if (check_window(p, window, sinks, &c, &w) != ATTN_OK) return 0;
+  if (!attn::window_hides(p->N, w.window, w.sinks)) return attn_bwd_workspace_bytes(p);
+  return ws_layout(p).d_bytes + attn::window_part_bytes(w, p->d);
+}
+
+int attn_window_bwd(const attn_params* p, int32_t window, int32_t sinks, const void* Q, const void* K, const void* V, const void* O, const void* dO, const float* LSE,
+                    void* dQ, void* dK, void* dV, void* workspace, size_t workspace_bytes) {
+  Checked c;
+  attn::WindowArgs w;
+  const int st = check_window(p, window, sinks, &c, &w);
+  if (st != ATTN_OK) return st;
+  if (!attn::window_hides(p->N, w.window, w.sinks))
+    return bwd_common(p, nullptr, 0, false, Q, K, V, O, dO, LSE, dQ, dK, dV, workspace, workspace_bytes);
+  if (!Q || !K || !V || !O || !dO || !LSE || !dQ || !dK || !dV) return ATTN_ERR_NULL;
+  if (!aligned16({Q, K, V, O, dO, dQ, dK, dV}) || ((uintptr_t)LSE & 3u) != 0) return ATTN_ERR_SHAPE;
+  const size_t rows = ws_layout(p).d_bytes;
+  if (workspace == nullptr || ((uintptr_t)workspace & 255u) != 0 || workspace_bytes < rows + attn::window_part_bytes(w, p->d)) return ATTN_ERR_WORKSPACE;
+  w.k.Q = Q; w.k.K = K; w.k.V = V; w.k.O = const_cast<void*>(O); w.k.LSE = const_cast<float*>(LSE);
+  w.k.dO = dO; w.k.dQ = dQ; w.k.dK = dK; w.k.dV = dV;
+  w.k.Dvec = (float*)workspace;
+  w.k.L2vec = w.k.Dvec + (size_t)p->B * p->H * w.k.Nr;
+  w.part = (float*)((char*)workspace + rows);
+  return attn::launch_window_bwd(w, c.dtype, c.d, c.dropout, c.stream) == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 
 int attn_bwd_timed(const attn_params* p, const uint8_t* block_mask, int32_t mask_block,

@@ -32,6 +32,17 @@ struct Library {
   decltype(&attn_blocksparse_bwd_workspace_bytes) sparse_workspace_bytes = nullptr;
 };
 Library lib;
+struct WindowLibrary {
+  decltype(&attn_window_fwd) fwd = nullptr;
+  decltype(&attn_window_bwd) bwd = nullptr;
+  decltype(&attn_window_bwd_workspace_bytes) workspace_bytes = nullptr;
+};
+WindowLibrary window_lib;
+// Of the three kinds of attention.
+enum Kind { kDense, kSparse, kWindow };
+const char* const kForwardNames[] = {"attn_fwd", "attn_blocksparse_fwd", "attn_window_fwd"};
+const char* const kBackwardNames[] = {"attn_bwd", "attn_blocksparse_bwd", "attn_window_bwd"};
+struct Window { int32_t window, sinks; };   // window 0: none
 bool alike(const at::Tensor& ref, const at::Tensor& t) {
   return t.sizes() == ref.sizes() && t.strides() == ref.strides() && t.device() == ref.device();
 }
@@ -91,6 +102,13 @@ Mask mask_args(PyObject* mask, PyObject* mask_block, int64_t H) {
   return r;
 }
 
+// window, sinks
+Window window_args(PyObject* const* a) {
+  const Window w = {clamped32(a[0]), clamped32(a[1])};
+  if (w.window < 1 || w.sinks < 0) raise(PyExc_ValueError, "window must be at least 1, and sinks must not be negative");
+  return w;
+}
+
 at::Tensor like(const at::Tensor& q, at::ScalarType type) {
   return at::empty_strided(q.sizes(), q.strides(), q.options().dtype(type));
 }
@@ -105,6 +123,8 @@ void expect_args(Py_ssize_t n, Py_ssize_t want) {
 struct Attention {
   attn_params p;            // pointers (stream, key lengths) are set again for each call
   at::Tensor key_lengths, block_mask;
+  Window w;
+  Kind kind() const { return w.window != 0 ? kWindow : (block_mask.defined() ? kSparse : kDense); }
 };
 
 attn_params on_current_stream(const Attention& a, const at::Tensor& q) {
@@ -137,16 +157,17 @@ using torch::autograd::variable_list;
 
 struct FlashAttention : torch::autograd::Function<FlashAttention> {
   static at::Tensor forward(AutogradContext* ctx, const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, const Attention& a) {
-    const bool sparse = a.block_mask.defined();
+    const Kind kind = a.kind();
     const attn_params p = on_current_stream(a, q);
     const at::Tensor out = like(q, q.scalar_type()), lse = at::empty(q.sizes().slice(0, 3), q.options().dtype(at::kFloat));
     const void *qp = q.data_ptr(), *kp = k.data_ptr(), *vp = v.data_ptr();
     void* op = out.data_ptr();
     float* lp = (float*)lse.data_ptr();
     check_status(without_gil([&] {
-      return sparse ? lib.sparse_fwd(&p, (const uint8_t*)a.block_mask.data_ptr(), 128, mask_stride(a.block_mask), qp, kp, vp, op, lp)
-                    : lib.fwd(&p, qp, kp, vp, op, lp);
-    }), sparse ? "attn_blocksparse_fwd" : "attn_fwd");
+      if (kind == kWindow) return window_lib.fwd(&p, a.w.window, a.w.sinks, qp, kp, vp, op, lp);
+      return kind == kSparse ? lib.sparse_fwd(&p, (const uint8_t*)a.block_mask.data_ptr(), 128, mask_stride(a.block_mask), qp, kp, vp, op, lp)
+                             : lib.fwd(&p, qp, kp, vp, op, lp);
+    }), kForwardNames[kind]);
     ctx->save_for_backward({q, k, v, out, lse});
     auto& data = ctx->saved_data;
     data["softmax_scale"] = (double)a.p.softmax_scale;
@@ -155,7 +176,11 @@ struct FlashAttention : torch::autograd::Function<FlashAttention> {
     data["seed"] = (int64_t)a.p.seed;
     data["offset"] = (int64_t)a.p.offset;
     if (a.key_lengths.defined()) data["key_lengths"] = a.key_lengths;
-    if (sparse) data["block_mask"] = a.block_mask;
+    if (kind == kSparse) data["block_mask"] = a.block_mask;
+    if (kind == kWindow) {
+      data["window"] = (int64_t)a.w.window;
+      data["sinks"] = (int64_t)a.w.sinks;
+    }
     return out;
   }
 
@@ -169,6 +194,7 @@ struct FlashAttention : torch::autograd::Function<FlashAttention> {
     Attention a = {};
     if (data.count("key_lengths")) a.key_lengths = data["key_lengths"].toTensor();
     if (data.count("block_mask")) a.block_mask = data["block_mask"].toTensor();
+    if (data.count("window")) a.w = {(int32_t)data["window"].toInt(), (int32_t)data["sinks"].toInt()};
     check_saved(q, k, v, d_out, a);
     a.p.B = (int32_t)q.size(0); a.p.H = (int32_t)q.size(1); a.p.N = (int32_t)q.size(2); a.p.d = (int32_t)q.size(3);
     a.p.dtype = q.scalar_type() == at::kHalf ? ATTN_FP16 : ATTN_BF16;
@@ -177,27 +203,29 @@ struct FlashAttention : torch::autograd::Function<FlashAttention> {
     a.p.dropout_p = (float)data["dropout_p"].toDouble();
     a.p.seed = (uint64_t)data["seed"].toInt();
     a.p.offset = (uint64_t)data["offset"].toInt();
-    const bool sparse = a.block_mask.defined();
+    const Kind kind = a.kind();
     const attn_params p = on_current_stream(a, q);
     at::Tensor g[3];
     for (at::Tensor& t : g) t = like(q, q.scalar_type());
-    const size_t need = sparse ? lib.sparse_workspace_bytes(&p) : lib.workspace_bytes(&p);
+    const size_t need = kind == kWindow ? window_lib.workspace_bytes(&p, a.w.window, a.w.sinks) : (kind == kSparse ? lib.sparse_workspace_bytes(&p) : lib.workspace_bytes(&p));
     const at::Tensor ws = at::empty({(int64_t)std::max<size_t>(need, 256)}, q.options().dtype(at::kByte));
     const float* lp = (const float*)lse.data_ptr();
     const int status =
-        sparse ? lib.sparse_bwd(&p, (const uint8_t*)a.block_mask.data_ptr(), 128, mask_stride(a.block_mask), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        kind == kWindow ? window_lib.bwd(&p, a.w.window, a.w.sinks, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), d_out.data_ptr(), lp, g[0].data_ptr(), g[1].data_ptr(),
+                                         g[2].data_ptr(), ws.data_ptr(), ws.numel())
+        : kind == kSparse ? lib.sparse_bwd(&p, (const uint8_t*)a.block_mask.data_ptr(), 128, mask_stride(a.block_mask), q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                 out.data_ptr(), d_out.data_ptr(), lp, g[0].data_ptr(), g[1].data_ptr(), g[2].data_ptr(), ws.data_ptr(), ws.numel())
                : lib.bwd(&p, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), d_out.data_ptr(), lp, g[0].data_ptr(), g[1].data_ptr(),
                          g[2].data_ptr(), ws.data_ptr(), ws.numel());
-    if (status != ATTN_OK) refused_in_backward([&] { check_status(status, sparse ? "attn_blocksparse_bwd" : "attn_bwd"); });
+    if (status != ATTN_OK) refused_in_backward([&] { check_status(status, kBackwardNames[kind]); });
     return {g[0], g[1], g[2], at::Tensor()};
   }
 };
 
-// attention(Q, K, V, softmax_scale, causal, dropout_p, seed, offset, key_lengths, block_mask) -> O, differentiable
+// attention(Q, K, V, softmax_scale, causal, dropout_p, seed, offset, key_lengths, block_mask[, window, sinks]) -> O, differentiable
 PyObject* py_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    expect_args(n, 10);
+    expect_args(n, n == 12 ? 12 : 10);
     const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]);
     same_layout(q, k);
     same_layout(q, v);
@@ -216,38 +244,46 @@ PyObject* py_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       Py_DECREF(block);
       at.block_mask = tensor(a[9]);
     }
+    if (n == 12) {
+      at.w = window_args(a + 10);
+      if (at.block_mask.defined()) raise(PyExc_ValueError, "a window and a block mask do not go together");
+      if (at::GradMode::is_enabled()) refuse_eager_graphs({&q, &k, &v});
+    }
     return wrap(FlashAttention::apply(q, k, v, at));
   });
 }
 
-// fwd(Q, K, V, <options>, out, lse[, block_mask, mask_block]) -> (O, LSE)
-PyObject* forward(PyObject* const* a, Py_ssize_t n, bool sparse) {
+// fwd(Q, K, V, <options>, out, lse[, block_mask, mask_block | window, sinks]) -> (O, LSE)
+PyObject* forward(PyObject* const* a, Py_ssize_t n, Kind kind) {
   return guarded([&]() -> PyObject* {
-    expect_args(n, 3 + kOptions + 2 + (sparse ? 2 : 0));
+    expect_args(n, 3 + kOptions + 2 + (kind != kDense ? 2 : 0));
     const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]);
     same_layout(q, k);
     same_layout(q, v);
     const attn_params p = make_params(a[0], options(a + 3));
     PyObject* const* r = a + 3 + kOptions;
     Mask m = {};
-    if (sparse) m = mask_args(r[2], r[3], q.size(1));
+    Window w = {};
+    if (kind == kSparse) m = mask_args(r[2], r[3], q.size(1));
+    if (kind == kWindow) w = window_args(r + 2);
     const at::Tensor out = r[0] != Py_None ? tensor(r[0]) : like(q, p.o_fp32 ? at::kFloat : q.scalar_type());
     const at::Tensor lse = r[1] != Py_None ? tensor(r[1]) : at::empty(q.sizes().slice(0, 3), q.options().dtype(at::kFloat));
     const void *qp = q.data_ptr(), *kp = k.data_ptr(), *vp = v.data_ptr();
     void* op = out.data_ptr();
     float* lp = (float*)lse.data_ptr();
     check_status(without_gil([&] {
-      return sparse ? lib.sparse_fwd(&p, m.ptr, m.block, m.stride_h, qp, kp, vp, op, lp) : lib.fwd(&p, qp, kp, vp, op, lp);
-    }), sparse ? "attn_blocksparse_fwd" : "attn_fwd");
+      if (kind == kWindow) return window_lib.fwd(&p, w.window, w.sinks, qp, kp, vp, op, lp);
+      return kind == kSparse ? lib.sparse_fwd(&p, m.ptr, m.block, m.stride_h, qp, kp, vp, op, lp) : lib.fwd(&p, qp, kp, vp, op, lp);
+    }), kForwardNames[kind]);
     return tuple({r[0] != Py_None ? Py_NewRef(r[0]) : wrap(out), r[1] != Py_None ? Py_NewRef(r[1]) : wrap(lse)});
   });
 }
 
-// bwd(Q, K, V, O, dO, LSE, <options>, workspace, allocate, dQ, dK, dV[, block_mask, mask_block]) -> (dQ, dK, dV);
+// bwd(Q, K, V, O, dO, LSE, <options>, workspace, allocate, dQ, dK, dV[, block_mask, mask_block | window, sinks]) -> (dQ, dK, dV);
 // allocate: dQ, dK and dV are made here, else they are the caller's
-PyObject* backward(PyObject* const* a, Py_ssize_t n, bool sparse) {
+PyObject* backward(PyObject* const* a, Py_ssize_t n, Kind kind) {
   return guarded([&]() -> PyObject* {
-    expect_args(n, 6 + kOptions + 5 + (sparse ? 2 : 0));
+    expect_args(n, 6 + kOptions + 5 + (kind != kDense ? 2 : 0));
     const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]), &go = tensor(a[4]);
     same_layout(q, k);
     same_layout(q, v);
@@ -255,7 +291,9 @@ PyObject* backward(PyObject* const* a, Py_ssize_t n, bool sparse) {
     const attn_params p = make_params(a[0], options(a + 6));
     PyObject* const* r = a + 6 + kOptions;
     Mask m = {};
-    if (sparse) m = mask_args(r[5], r[6], q.size(1));
+    Window w = {};
+    if (kind == kSparse) m = mask_args(r[5], r[6], q.size(1));
+    if (kind == kWindow) w = window_args(r + 5);
     const bool allocate = truth(r[1]);
     at::Tensor g[3];
     void* gp[3];
@@ -267,7 +305,7 @@ PyObject* backward(PyObject* const* a, Py_ssize_t n, bool sparse) {
     if (r[0] != Py_None) {
       ws = tensor(r[0]);
     } else {
-      const size_t need = sparse ? lib.sparse_workspace_bytes(&p) : lib.workspace_bytes(&p);
+      const size_t need = kind == kWindow ? window_lib.workspace_bytes(&p, w.window, w.sinks) : (kind == kSparse ? lib.sparse_workspace_bytes(&p) : lib.workspace_bytes(&p));
       ws = at::empty({(int64_t)std::max<size_t>(need, 256)}, q.options().dtype(at::kByte));
     }
     const size_t ws_bytes = (size_t)ws.numel() * ws.element_size();
@@ -275,19 +313,22 @@ PyObject* backward(PyObject* const* a, Py_ssize_t n, bool sparse) {
     const float* lp = (const float*)data(a[5]);
     void* wp = ws.data_ptr();
     check_status(without_gil([&] {
-      return sparse ? lib.sparse_bwd(&p, m.ptr, m.block, m.stride_h, qp, kp, vp, op, gop, lp, gp[0], gp[1], gp[2], wp, ws_bytes)
+      if (kind == kWindow) return window_lib.bwd(&p, w.window, w.sinks, qp, kp, vp, op, gop, lp, gp[0], gp[1], gp[2], wp, ws_bytes);
+      return kind == kSparse ? lib.sparse_bwd(&p, m.ptr, m.block, m.stride_h, qp, kp, vp, op, gop, lp, gp[0], gp[1], gp[2], wp, ws_bytes)
                     : lib.bwd(&p, qp, kp, vp, op, gop, lp, gp[0], gp[1], gp[2], wp, ws_bytes);
-    }), sparse ? "attn_blocksparse_bwd" : "attn_bwd");
+    }), kBackwardNames[kind]);
     PyObject* t[3];
     for (int i = 0; i < 3; ++i) t[i] = allocate ? wrap(g[i]) : Py_NewRef(r[2 + i]);
     return tuple({t[0], t[1], t[2]});
   });
 }
 
-PyObject* py_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) { return forward(a, n, false); }
-PyObject* py_sparse_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) { return forward(a, n, true); }
-PyObject* py_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) { return backward(a, n, false); }
-PyObject* py_sparse_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) { return backward(a, n, true); }
+PyObject* py_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) { return forward(a, n, kDense); }
+PyObject* py_sparse_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) { return forward(a, n, kSparse); }
+PyObject* py_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) { return backward(a, n, kDense); }
+PyObject* py_sparse_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) { return backward(a, n, kSparse); }
+PyObject* py_window_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) { return forward(a, n, kWindow); }
+PyObject* py_window_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) { return backward(a, n, kWindow); }
 
 // attach(AttnError, address of attn_fwd, attn_bwd, attn_bwd_workspace_bytes, and the three block-sparse ones)
 PyObject* py_attach(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -308,7 +349,23 @@ PyObject* py_attach(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// attach_window(address of attn_window_fwd, attn_window_bwd, attn_window_bwd_workspace_bytes)
+PyObject* py_attach_window(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 3) raise(PyExc_TypeError, "attach_window() takes three addresses");
+    WindowLibrary l;
+    l.fwd = (decltype(l.fwd))low64(a[0]);
+    l.bwd = (decltype(l.bwd))low64(a[1]);
+    l.workspace_bytes = (decltype(l.workspace_bytes))low64(a[2]);
+    window_lib = l;
+    Py_RETURN_NONE;
+  });
+}
+
 const PyMethodDef own_methods[] = {
+    {"attach_window", (PyCFunction)(void*)py_attach_window, METH_FASTCALL, nullptr},
+    {"window_fwd", (PyCFunction)(void*)py_window_fwd, METH_FASTCALL, nullptr},
+    {"window_bwd", (PyCFunction)(void*)py_window_bwd, METH_FASTCALL, nullptr},
     {"attach", (PyCFunction)(void*)py_attach, METH_FASTCALL, nullptr},
     {"attention", (PyCFunction)(void*)py_attention, METH_FASTCALL, nullptr},
     {"fwd", (PyCFunction)(void*)py_fwd, METH_FASTCALL, nullptr},

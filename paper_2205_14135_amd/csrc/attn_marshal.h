@@ -67,6 +67,16 @@ inline uint64_t low64(PyObject* o) {   // int(o) & (2^64 - 1)
   return v;
 }
 
+inline int32_t clamped32(PyObject* o) {   // an integer, kept within 32 bits
+  PyObject* i = PyNumber_Index(o);
+  if (i == nullptr) throw Raised();
+  int beyond = 0;
+  const long long v = PyLong_AsLongLongAndOverflow(i, &beyond);
+  Py_DECREF(i);
+  if (beyond != 0) return beyond > 0 ? INT32_MAX : INT32_MIN;
+  return v > INT32_MAX ? INT32_MAX : (v < INT32_MIN ? INT32_MIN : (int32_t)v);
+}
+
 // The library call itself runs without the interpreter lock.
 template <typename F> int without_gil(F&& f) {
   PyThreadState* s = PyEval_SaveThread();
@@ -105,6 +115,9 @@ template <typename F> [[noreturn]] void refused_in_backward(F&& set) {
   PyGILState_Release(gil);
   throw e;
 }
+
+// Of a forward pass under capture (attn_paged_marshal.cpp).
+void refuse_eager_graphs(std::initializer_list<const at::Tensor*> tensors);
 
 // The functions of attn_paged_marshal.cpp, ended by an empty entry.
 extern PyMethodDef paged_methods[];

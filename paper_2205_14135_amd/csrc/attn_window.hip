@@ -1,0 +1,407 @@
+// Forward pass and dQ of attention with a sliding window and first tokens that stay visible, gfx950.
+//
+// Key j is visible to query i iff j <= i and (i - j < window or j < sinks).  The arithmetic is that of the causal kernels (attn_fwd.hip, attn_bwd.hip); a block of 128 rows sweeps the
+// tiles of 64 keys that hold sinks and those from the first one that its first row's window reaches to the diagonal: (window + 128) / 64 + 1 of them and the sinks', whatever the length.  Blocks cost
+// the same but for the first of a head, so that they are dealt out in order, neighbours to the same XCD, whose L2 has loaded most of their keys already.
+// Masks are looked at in the tiles that the edges cross only, the diagonal, the window's far edge and the last sink; wavefronts whose 32 rows see nothing of a tile skip it.
+#include "attn_window.h"
+
+#include "attn_tiles.h"
+
+namespace attn {
+namespace {
+
+constexpr int TILE = 64;   // keys
+
+// The tiles of a block of rows r0 .. r0 + BR - 1, in order: those of the sinks, then those of the window.  len: keys that there are.
+struct WindowTiles {
+  int at, sink_end, first, limit;
+  template <int BR> __device__ __forceinline__ void init(const WindowArgs& a, int r0, int len) {
+    const int lo = max(r0 - a.window + 1, 0);   // the first key in reach
+    first = lo / TILE;
+    limit = r0 >= len ? 0 : (min(r0 + BR, len) + TILE - 1) / TILE;
+    sink_end = min((a.sinks + TILE - 1) / TILE, first);
+    at = sink_end > 0 ? 0 : first;
+    if (limit == 0) at = 0;
+  }
+  __device__ __forceinline__ int next() {   // -1: no more
+    if (at >= limit) return -1;
+    const int t = at++;
+    if (at == sink_end) at = first;
+    return t;
+  }
+};
+// Whether rows q0 .. q0 + 31 see any of the tile's keys from k0 on.
+__device__ __forceinline__ bool wave_sees(const WindowArgs& a, int k0, int q0) { return k0 <= q0 + 31 && (q0 - k0 < a.window + TILE - 1 || k0 < a.sinks); }
+// The far edge: keys that lie a window or more before the row and are no sinks.  (The near one and the length are the caller's.)
+__device__ __forceinline__ void hide_far(const WindowArgs& a, f32x16 (&s)[2], int k0, int q0, int qi, int g) {
+  if (q0 + 31 - k0 >= a.window && k0 + TILE > a.sinks) {
+    const int first = qi - a.window + 1;   // of the row's window
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = k0 + 32 * kb + 8 * (i >> 2) + 4 * g + (i & 3);
+        if (key < first && key >= a.sinks) s[kb][i] = -INFINITY;
+      }
+  }
+}
+
+template <typename T, int D, bool DROPOUT>
+__global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void window_fwd_kernel(const WindowArgs w) {
+  typedef typename Vec<T>::x8 T8;
+  constexpr int KK = D / 16, DB = D / 32, BR = 128, PF = 4;
+  typedef T Tile[TILE * D];
+  __shared__ __attribute__((aligned(16))) Tile Ks[2], Vs[2];
+  const KArgs& a = w.k;
+  args_at_once(a);
+  const int item = xcd_item(a.n_items, a.chunk);
+  if (item < 0) return;
+  const int bh = dealt_head(a, item / a.T), qt = item % a.T;
+  const int b = bh / a.H, h = bh % a.H;
+  const int64_t head_off = (int64_t)b * a.sb + (int64_t)h * a.sh;
+  const T* __restrict__ Qg = (const T*)a.Q + head_off;
+  const T* __restrict__ Kg = (const T*)a.K + head_off;
+  const T* __restrict__ Vg = (const T*)a.V + head_off;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 31, g = lane >> 5;
+  const int q0 = qt * BR + wave * 32;
+  const bool row_ok = q0 + r < a.N;   // (lanes beyond a ragged end work on a copy of the last row and store nothing)
+  const int qi = min(q0 + r, a.N - 1);
+
+  T8 qf[KK];   // Q^T fragments (B operand): query qi, d = 16 kk + 8 g .. +7
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) {
+    if (D == 32 && 16 * kk + 8 * g >= a.dvalid) {   // head dimension 16: the upper columns are zeros
+#pragma unroll
+      for (int e = 0; e < 8; ++e) qf[kk][e] = (T)0.f;
+    } else {
+      qf[kk] = *(const T8*)(Qg + (int64_t)qi * a.sn + 16 * kk + 8 * g);
+    }
+  }
+  f32x16 o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x4 lr_run = {0.f, 0.f, 0.f, 0.f};
+  int calm = kFirstTile;
+  const T8 ones = row_sum_ones<T>();
+
+  const int len = a.klen ? min(max(a.klen[b], 0), a.N) : a.N;
+  WindowTiles it;
+  it.init<BR>(w, qt * BR, len);
+  TrOffsets<D> tro;
+  tro.init();
+  TileAsync<T, D, 4> dma;
+  dma.init(a.sn, wave, D == 32 ? a.dvalid : D);
+  if (D == 32 && a.dvalid < D) {   // the copies leave columns >= 16 of the tile buffers untouched
+    zero_tiles(&Ks[0][0], 2 * TILE * D);
+    zero_tiles(&Vs[0][0], 2 * TILE * D);
+    __syncthreads();
+  }
+  const float c = a.scale_log2;
+  int jt = it.next(), buf = 0;
+  if (jt >= 0) {
+    dma.copy_rows(Kg, a.sn, jt * TILE, a.N, Ks[0]);
+    dma.copy_rows(Vg, a.sn, jt * TILE, a.N, Vs[0]);
+  }
+  wait_async_copies();
+  __syncthreads();   // the first tile has landed, and so have the Q fragments
+  asm volatile("" ::"s"(c));
+  uint32_t k_off[KK];   // byte offsets of this lane's K fragments in a tile, kept whole
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) {
+    k_off[kk] = lds_addr(&Ks[0][0]) + (uint32_t)(lds_off<D>(r, 2 * kk + g) * sizeof(T));
+    asm volatile("" : "+v"(k_off[kk]));
+  }
+  while (jt >= 0) {
+    const int jn = it.next();
+    if (jn >= 0) {   // the next tile streams into the other buffer while this one is used
+      dma.copy_rows(Kg, a.sn, jn * TILE, a.N, Ks[buf ^ 1]);
+      dma.copy_rows(Vg, a.sn, jn * TILE, a.N, Vs[buf ^ 1]);
+    }
+    const T* Vt = Vs[buf];
+    const int k0 = jt * TILE;
+    if (wave_sees(w, k0, q0)) {
+      f32x16 s[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+      {   // S^T = K Q^T; operand reads run PF fragments ahead of their MFMA
+        auto k_frag = [&](int f) {   // f = 2 kk + kb
+          const auto* p = (const __attribute__((address_space(3))) T8*)(k_off[f >> 1] + (uint32_t)(buf * TILE * D * sizeof(T)));
+          return p[32 * (f & 1) * D / 8];
+        };
+        T8 ring[PF];
+#pragma unroll
+        for (int f = 0; f < PF; ++f) ring[f] = k_frag(f);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = 0; f < 2 * KK; ++f) {
+          const T8 cur = ring[f % PF];
+          s[f & 1] = mfma32(cur, qf[f >> 1], s[f & 1]);
+          if (f + PF < 2 * KK) ring[f % PF] = k_frag(f + PF);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      hide_far(w, s, k0, q0, qi, g);
+      T8 pf[4];
+      softmax_tile_lane_query<T, DB, true, DROPOUT, D == 128>(a, s, o, pf, m_run, l_run, lr_run, calm, ones, c, k0, q0, qi, len, g, bh);
+      {   // O^T += V^T P^T
+        auto v_frag = [&](int f) {   // f = DB cc + db: consecutive MFMAs hit different accumulators
+          const T* base = Vt + 16 * (f / DB) * D;
+          return tr_frag<T8>(base + tro.off[f % DB][0], base + tro.off[f % DB][1]);
+        };
+        T8 ring[PF];
+#pragma unroll
+        for (int f = 0; f < PF; ++f) ring[f] = v_frag(f);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = 0; f < 4 * DB; ++f) {
+          const T8 cur = ring[f % PF];
+          o[f % DB] = mfma32(cur, pf[f / DB], o[f % DB]);
+          if (f + PF < 4 * DB) ring[f % PF] = v_frag(f + PF);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    wait_async_copies();
+    __syncthreads();   // the next tile has landed, and everyone is done with this buffer
+    jt = jn;
+    buf ^= 1;
+  }
+
+  const float l_sum = l_run + xchg32(l_run);
+  const float lr_sum = lr_run[0];
+  const float l_tot = qi < len ? l_sum : 0.f;   // padding rows: O = 0, LSE = -inf
+  const float inv = (l_tot > 0.f && lr_sum > 0.f) ? (DROPOUT ? a.keep_scale : 1.f) / lr_sum : (l_tot == l_tot ? 0.f : l_tot);   // (a row of NaN stays one)
+  if (g == 0 && row_ok)
+    a.LSE[(int64_t)bh * a.N + qi] = l_tot > 0.f ? (m_run + __builtin_amdgcn_logf(l_tot)) * 0.6931471805599453f : -INFINITY;
+  if (a.o_fp32) {
+    float* Og = (float*)a.O + head_off + (int64_t)qi * a.sn;
+    if (row_ok) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = o[db][4 * i4 + e] * inv;
+          if (D != 32 || 8 * i4 + 4 * g < a.dvalid) *(f32x4*)(Og + 32 * db + 8 * i4 + 4 * g) = v;
+        }
+    }
+  } else {   // through the (now idle) tile buffers
+    T* stage = wave < 2 ? &Ks[0][0] + wave * 32 * D : &Vs[0][0] + (wave - 2) * 32 * D;
+    store_rows_coalesced<T, D>(stage, (T*)a.O + head_off + (int64_t)q0 * a.sn, a.sn, o, inv, a.N - q0, D == 32 ? a.dvalid : D);
+  }
+}
+
+// dQ, and -D and the row statistic in base 2 for the dK/dV kernels, as in attn_bwd.hip.
+template <typename T, int D, bool DROPOUT>
+__global__ __launch_bounds__(256, 2) void window_dq_kernel(const WindowArgs w) {
+  typedef typename Vec<T>::x8 T8;
+  constexpr int KK = D / 16, DB = D / 32, BR = 128, PF = 4;
+  __shared__ __attribute__((aligned(16))) T Ks[2 * TILE * D];
+  __shared__ __attribute__((aligned(16))) T Vs[2 * TILE * D];
+  const KArgs& a = w.k;
+  args_at_once(a);
+  const int item = xcd_item(a.n_items, a.chunk);
+  if (item < 0) return;
+  const int bh = dealt_head(a, item / a.T), qt = item % a.T;
+  const int b = bh / a.H, h = bh % a.H;
+  const int64_t head_off = (int64_t)b * a.sb + (int64_t)h * a.sh;
+  const T* __restrict__ Kg = (const T*)a.K + head_off;
+  const T* __restrict__ Vg = (const T*)a.V + head_off;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 31, g = lane >> 5;
+  const int q0 = qt * BR + wave * 32;
+  const bool row_ok = q0 + r < a.N;
+  const int qi = min(q0 + r, a.N - 1);
+
+  T8 qf[KK], gf[KK];   // Q^T and dO^T fragments of this lane's query
+  float d_part = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) {
+    const int64_t off = head_off + (int64_t)qi * a.sn + 16 * kk + 8 * g;
+    if (D == 32 && 16 * kk + 8 * g >= a.dvalid) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) { qf[kk][e] = (T)0.f; gf[kk][e] = (T)0.f; }
+      continue;
+    }
+    qf[kk] = *(const T8*)((const T*)a.Q + off);
+    gf[kk] = *(const T8*)((const T*)a.dO + off);
+    if (a.o_fp32) {
+      const f32x4 o0 = *(const f32x4*)((const float*)a.O + off);
+      const f32x4 o1 = *(const f32x4*)((const float*)a.O + off + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) d_part += (float)gf[kk][e] * o0[e] + (float)gf[kk][4 + e] * o1[e];
+    } else {
+      const T8 o = *(const T8*)((const T*)a.O + off);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d_part += (float)gf[kk][e] * (float)o[e];
+    }
+  }
+  const float lse = a.LSE[(int64_t)bh * a.N + qi];
+  const float l2 = (lse == -INFINITY || !row_ok) ? INFINITY : lse * 1.4426950408889634f;
+  const float neg_d = row_ok ? -(d_part + xchg32(d_part)) : 0.f;   // -D_i
+  if (g == 0) {   // (the scratch is padded to whole blocks: this workgroup writes all of its block)
+    a.Dvec[(int64_t)bh * a.Nr + q0 + r] = neg_d;
+    a.L2vec[(int64_t)bh * a.Nr + q0 + r] = l2;
+  }
+  f32x16 dq[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dq[db][i] = 0.f;
+
+  const int len = a.klen ? min(max(a.klen[b], 0), a.N) : a.N;
+  WindowTiles it;
+  it.init<BR>(w, qt * BR, len);
+  TrOffsets<D> tro;
+  tro.init();
+  TileAsync<T, D, 4> dma;
+  dma.init(a.sn, wave, D == 32 ? a.dvalid : D);
+  if (D == 32 && a.dvalid < D) {
+    zero_tiles(Ks, 2 * TILE * D);
+    zero_tiles(Vs, 2 * TILE * D);
+    __syncthreads();
+  }
+  const float c = a.scale_log2;
+  int jt = it.next(), buf = 0;
+  if (jt >= 0) {
+    dma.copy_rows(Kg, a.sn, jt * TILE, a.N, Ks);
+    dma.copy_rows(Vg, a.sn, jt * TILE, a.N, Vs);
+  }
+  wait_async_copies();
+  __syncthreads();
+  while (jt >= 0) {
+    const int jn = it.next();
+    if (jn >= 0) {
+      dma.copy_rows(Kg, a.sn, jn * TILE, a.N, Ks + (buf ^ 1) * TILE * D);
+      dma.copy_rows(Vg, a.sn, jn * TILE, a.N, Vs + (buf ^ 1) * TILE * D);
+    }
+    const T* Kt = Ks + buf * TILE * D;
+    const T* Vt = Vs + buf * TILE * D;
+    const int k0 = jt * TILE;
+    if (wave_sees(w, k0, q0)) {
+      f32x16 s[2], dp[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[kb][i] = 0.f;
+          dp[kb][i] = DROPOUT ? 0.f : neg_d;   // without dropout the product starts from -D and ends as dP - D
+        }
+      // S^T = K Q^T and dP^T = V dO^T as one stream
+      auto kv_frag = [&](int f) {   // f = 4 kk + 2 kb + (0: K, 1: V)
+        const int off = lds_off<D>(32 * ((f >> 1) & 1) + r, 2 * (f >> 2) + g);
+        return *(const T8*)(((f & 1) ? Vt : Kt) + off);
+      };
+      {
+        T8 ring[PF];
+#pragma unroll
+        for (int f = 0; f < PF; ++f) ring[f] = kv_frag(f);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = 0; f < 4 * KK; ++f) {
+          const T8 cur = ring[f % PF];
+          const int kk = f >> 2, kb = (f >> 1) & 1;
+          if (f & 1) dp[kb] = mfma32(cur, gf[kk], dp[kb]);
+          else s[kb] = mfma32(cur, qf[kk], s[kb]);
+          if (f + PF < 4 * KK) ring[f % PF] = kv_frag(f + PF);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      hide_far(w, s, k0, q0, qi, g);
+      if (k0 + TILE - 1 > q0 || k0 + TILE > len) {
+        const int last = min(qi, len - 1);   // last visible key of this row
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (k0 + 32 * kb + 8 * (i >> 2) + 4 * g + (i & 3) > last) s[kb][i] = -INFINITY;
+      }
+      KeepLQ kq = {};
+      if constexpr (DROPOUT) kq = keep_tile_lane_query(k0, qi, bh, g, a.offset_lo, a.seed_lo, a.seed_hi);
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = 4 * i4 + e;
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], c, -l2));
+            float dpv = dp[kb][i];
+            if constexpr (DROPOUT) dpv = dropped(kq.w[kb][i4], e, a.drop_thr) ? neg_d : __builtin_fmaf(dpv, a.keep_scale, neg_d);
+            s[kb][i] = p * dpv;
+          }
+      T8 dsf[4];
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc)
+#pragma unroll
+        for (int t = 0; t < 8; ++t) dsf[cc][t] = (T)s[cc >> 1][8 * (cc & 1) + t];
+      auto kt_frag = [&](int f) {   // f = DB cc + db
+        const T* base = Kt + 16 * (f / DB) * D;
+        return tr_frag<T8>(base + tro.off[f % DB][0], base + tro.off[f % DB][1]);
+      };
+      {   // dQ^T += K^T dS^T
+        T8 ring[PF];
+#pragma unroll
+        for (int f = 0; f < PF; ++f) ring[f] = kt_frag(f);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = 0; f < 4 * DB; ++f) {
+          const T8 cur = ring[f % PF];
+          dq[f % DB] = mfma32(cur, dsf[f / DB], dq[f % DB]);
+          if (f + PF < 4 * DB) ring[f % PF] = kt_frag(f + PF);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    wait_async_copies();
+    __syncthreads();
+    jt = jn;
+    buf ^= 1;
+  }
+  T* stage = wave < 2 ? Ks + wave * 32 * D : Vs + (wave - 2) * 32 * D;
+  store_rows_coalesced<T, D>(stage, (T*)a.dQ + head_off + (int64_t)q0 * a.sn, a.sn, dq, a.tau, a.N - q0, D == 32 ? a.dvalid : D);
+}
+
+void set_items(KArgs& k, int blocks) {
+  k.n_items = k.B * k.H * blocks;
+  k.chunk = (k.n_items + kXcds - 1) / kXcds;
+}
+template <typename T, int D> int launch_fwd(WindowArgs a, bool dropout, hipStream_t s) {
+  set_items(a.k, a.k.T);
+  const dim3 grid(kXcds * a.k.chunk), block(256);
+  if (dropout) hipLaunchKernelGGL((window_fwd_kernel<T, D, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((window_fwd_kernel<T, D, false>), grid, block, 0, s, a);
+  return (int)hipGetLastError();
+}
+template <typename T, int D> int launch_dq(WindowArgs a, bool dropout, hipStream_t s) {
+  set_items(a.k, a.k.T);
+  const dim3 grid(kXcds * a.k.chunk), block(256);
+  if (dropout) hipLaunchKernelGGL((window_dq_kernel<T, D, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((window_dq_kernel<T, D, false>), grid, block, 0, s, a);
+  return (int)hipGetLastError();
+}
+
+}  // namespace
+
+int launch_window_fwd(const WindowArgs& a, int dtype, int d, bool dropout, hipStream_t s) {
+  if (d == 32) return dtype == 0 ? launch_fwd<_Float16, 32>(a, dropout, s) : launch_fwd<__bf16, 32>(a, dropout, s);
+  if (d == 64) return dtype == 0 ? launch_fwd<_Float16, 64>(a, dropout, s) : launch_fwd<__bf16, 64>(a, dropout, s);
+  return dtype == 0 ? launch_fwd<_Float16, 128>(a, dropout, s) : launch_fwd<__bf16, 128>(a, dropout, s);
+}
+int launch_window_bwd(const WindowArgs& a, int dtype, int d, bool dropout, hipStream_t s) {
+  int e;
+  if (d == 32) e = dtype == 0 ? launch_dq<_Float16, 32>(a, dropout, s) : launch_dq<__bf16, 32>(a, dropout, s);
+  else if (d == 64) e = dtype == 0 ? launch_dq<_Float16, 64>(a, dropout, s) : launch_dq<__bf16, 64>(a, dropout, s);
+  else e = dtype == 0 ? launch_dq<_Float16, 128>(a, dropout, s) : launch_dq<__bf16, 128>(a, dropout, s);
+  return e != 0 ? e : launch_window_dkv(a, dtype, d, dropout, s);
+}
+
+}  // namespace attn
