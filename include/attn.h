@@ -436,6 +436,14 @@ size_t attn_paged_workspace_bytes(const attn_paged_params* p);
 int attn_paged_fwd(const attn_paged_params* p, const void* Q, const void* k_cache, const void* v_cache, void* O, float* LSE, void* workspace,
                    size_t workspace_bytes);
 
+/*
+ * The same with a sliding window (p->causal must be set): a new token at position i sees the keys at positions j <= i with i - j < window or j < sinks.  window >= 1, sinks >= 0.  Of a
+ * sequence's pages only those are read that hold a key that one of its new tokens sees; the others may belong to another sequence by now, or their numbers be none.  Workspace as
+ * for attn_paged_fwd.
+ */
+int attn_paged_window_fwd(const attn_paged_params* p, int32_t window, int32_t sinks, const void* Q, const void* k_cache, const void* v_cache, void* O, float* LSE,
+                          void* workspace, size_t workspace_bytes);
+
 /* Caches of one or more layers, [layers, pages, Hk, page_size, d]. */
 typedef struct {
   int32_t layers, pages, Hk, page_size, d;

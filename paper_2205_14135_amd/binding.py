@@ -25,7 +25,7 @@ SYMBOLS = (
     "attn_blocksparse_bwd", "attn_bwd_timed", "attn_debug_dropout_mask", "attn_debug_mfma_rate", "attn_debug_kernel_choice", "attn_debug_bwd_kernel", "attn_debug_set_variant", "attn_strerror",
     "attn_version", "attn_rotary", "attn_paged_append", "attn_paged_workspace_bytes", "attn_paged_fwd", "attn_paged_copy",
     "attn_norm_rotary", "attn_norm_rotary_bwd_workspace_bytes", "attn_norm_rotary_bwd", "attn_paged_norm_append",
-    "attn_window_fwd", "attn_window_bwd_workspace_bytes", "attn_window_bwd",
+    "attn_window_fwd", "attn_window_bwd_workspace_bytes", "attn_window_bwd", "attn_paged_window_fwd",
 )
 
 
@@ -118,6 +118,7 @@ def _attach_paged(lib: ctypes.CDLL) -> None:
         "attn_rotary", "attn_paged_append", "attn_paged_workspace_bytes", "attn_paged_fwd", "attn_paged_copy")))
     _marshal.attach_norm(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
         "attn_norm_rotary", "attn_norm_rotary_bwd_workspace_bytes", "attn_norm_rotary_bwd", "attn_paged_norm_append")))
+    _marshal.attach_paged_window(ctypes.cast(lib.attn_paged_window_fwd, ctypes.c_void_p).value)
 
 
 def load() -> ctypes.CDLL:
@@ -172,6 +173,8 @@ def load() -> ctypes.CDLL:
     lib.attn_paged_workspace_bytes.restype = sz
     lib.attn_paged_fwd.argtypes = [ctypes.POINTER(PagedParams)] + [vp] * 5 + [vp, sz]
     lib.attn_paged_fwd.restype = ctypes.c_int
+    lib.attn_paged_window_fwd.argtypes = [ctypes.POINTER(PagedParams), i32, i32] + [vp] * 5 + [vp, sz]
+    lib.attn_paged_window_fwd.restype = ctypes.c_int
     lib.attn_paged_copy.argtypes = [ctypes.POINTER(PagedCopyParams), vp, vp, vp, i64]
     lib.attn_paged_copy.restype = ctypes.c_int
     lib.attn_norm_rotary.argtypes = [ctypes.POINTER(RotaryParams), ctypes.POINTER(NormSpec), ctypes.POINTER(RotaryTensor), i32]
@@ -436,14 +439,19 @@ def attn_paged_workspace(Q, k_cache, sequences: int) -> torch.Tensor:
 
 
 def attn_paged_fwd(Q, k_cache, v_cache, block_table, lengths, query_starts=None, *, softmax_scale, causal=True, out=None, lse=None,
-                   workspace=None) -> Tuple[torch.Tensor, torch.Tensor]:
+                   workspace=None, window=None, sinks=0) -> Tuple[torch.Tensor, torch.Tensor]:
     """O [T,Hq,d], LSE [Hq,T]: attention of the new tokens of every sequence over its pages, the new tokens (see attn_paged_append) among them.
 
     The arguments are those of attn_paged_append; Hq is a multiple of Hk.  causal: a token sees its own position and those before it, else all of its
-    sequence.  A row that sees no key gets O = 0, LSE = -inf.  Outputs and workspace are allocated with torch unless given; rows of no sequence
+    sequence.  window (causal only): a token sees the last `window` keys up to its own, and the first `sinks` of its sequence; pages without a key
+    that a new token sees are not read.  A row that sees no key gets O = 0, LSE = -inf.  Outputs and workspace are allocated with torch unless given; rows of no sequence
     are left as they were (unspecified where the output is made here).  Runs on torch's current stream."""
     if _lib is None:
         load()
+    if window is not None:
+        return _marshal.paged_window_fwd(Q, k_cache, v_cache, block_table, lengths, query_starts, softmax_scale, causal, out, lse, workspace, window, sinks)
+    if sinks != 0:
+        raise ValueError("sinks are of no use without a window")
     return _marshal.paged_fwd(Q, k_cache, v_cache, block_table, lengths, query_starts, softmax_scale, causal, out, lse, workspace)
 
 

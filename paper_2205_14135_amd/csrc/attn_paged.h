@@ -111,6 +111,7 @@ struct PagedCall {
   int slots;              // workgroups that share the work
   float scale_log2;       // tau * log2(e)
   double longest_line;    // no rising starts make more of the line (attn_paged_line.h) than this
+  int window, sinks;      // a token sees the last `window` keys up to its own, and the first `sinks` (window 0: all up to its own)
 };
 
 // How attn_paged_fwd runs: blocks of 32 rows, a wavefront each (attn_paged_one.hip), or of 128 or 256 (attn_paged_rows.hip), and the workgroups that share the work.

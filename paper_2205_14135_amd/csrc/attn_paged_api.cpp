@@ -295,12 +295,15 @@ size_t attn_paged_workspace_bytes(const attn_paged_params* p) {
   return check_paged(p, &c, &shape) == ATTN_OK ? attn::paged_workspace_bytes(p->d) : 0;
 }
 
-int attn_paged_fwd(const attn_paged_params* p, const void* Q, const void* k_cache, const void* v_cache, void* O, float* LSE, void* workspace,
-                   size_t workspace_bytes) {
+// window 0: none
+static int paged_fwd(const attn_paged_params* p, int32_t window, int32_t sinks, const void* Q, const void* k_cache, const void* v_cache, void* O, float* LSE, void* workspace,
+                     size_t workspace_bytes) {
   attn::PagedCall c;
   attn::PagedShape shape;
   int st = check_paged(p, &c, &shape);
   if (st != ATTN_OK) return st;
+  c.window = window;
+  c.sinks = sinks;
   st = check_batch_pointers(c.b);
   if (st != ATTN_OK) return st;
   if (!Q || !k_cache || !v_cache || !O || !LSE) return ATTN_ERR_NULL;
@@ -312,6 +315,19 @@ int attn_paged_fwd(const attn_paged_params* p, const void* Q, const void* k_cach
   c.part = (float*)workspace;
   const int e = shape.rows == 32 ? attn::launch_paged_one(c, p->dtype, (hipStream_t)p->stream) : attn::launch_paged_rows(c, p->dtype, (hipStream_t)p->stream);
   return e == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
+}
+
+int attn_paged_fwd(const attn_paged_params* p, const void* Q, const void* k_cache, const void* v_cache, void* O, float* LSE, void* workspace,
+                   size_t workspace_bytes) {
+  return paged_fwd(p, 0, 0, Q, k_cache, v_cache, O, LSE, workspace, workspace_bytes);
+}
+
+int attn_paged_window_fwd(const attn_paged_params* p, int32_t window, int32_t sinks, const void* Q, const void* k_cache, const void* v_cache, void* O, float* LSE,
+                          void* workspace, size_t workspace_bytes) {
+  if (p == nullptr) return ATTN_ERR_NULL;
+  if (p->causal == 0 || window < 1 || sinks < 0) return ATTN_ERR_WINDOW;
+  // (a cache holds no more than 2^30 positions of a sequence)
+  return paged_fwd(p, window, sinks < (1 << 30) ? sinks : 1 << 30, Q, k_cache, v_cache, O, LSE, workspace, workspace_bytes);
 }
 
 int attn_paged_copy(const attn_paged_copy_params* p, void* k_cache, void* v_cache, const int32_t* pairs, int64_t n_pairs) {

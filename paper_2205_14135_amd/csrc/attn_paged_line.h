@@ -14,8 +14,10 @@ namespace attn {
 // How a kernel divides its line.  BR: rows of a block.  KEYS: of a tile.  ITEM: what an item costs beside its keys, in keys (Q, the wait for its first tile, its end); a piece costs
 // as much, and a join.  SLACK: keys that a cut is moved by to an end of its item.  SPREAD: a stretch has at least the square root of SPREAD times the longest item's keys, so that joining the pieces takes no longer than making one:
 // with k keys in each of n / k pieces the kernel takes c k for a piece, the join C n / k, and the sum is least at k^2 = n C / c.
-template <int BR_, int KEYS_, int ITEM_, int SLACK_, int SPREAD_> struct Division {
+// WINDOW: tokens see a window of keys and sinks only.
+template <int BR_, int KEYS_, int ITEM_, int SLACK_, int SPREAD_, bool WINDOW_ = false> struct Division {
   static constexpr int BR = BR_, KEYS = KEYS_, ITEM = ITEM_, SLACK = SLACK_, SPREAD = SPREAD_;
+  static constexpr bool WINDOW = WINDOW_;
 };
 // A sequence of the batch, every number taken from device memory forced into its range.
 struct Sequence {
@@ -38,6 +40,14 @@ template <class DIV> __device__ __forceinline__ Sequence sequence_of(const Paged
   s.blocks = (s.rows + DIV::BR - 1) / DIV::BR;
   s.a = (double)c.G * ((c.causal ? max(min(base, L), 0) : L) + DIV::ITEM);
   s.step = c.causal ? DIV::BR : 0;
+  if constexpr (DIV::WINDOW) {
+    // Blocks of a sequence that is longer than the window see about as many keys each: the window of the first row, the rows behind it, the sinks, and what tiles are rounded by.
+    const int64_t reach = (int64_t)c.window + c.sinks + DIV::BR / c.G + 2 * DIV::KEYS;
+    if (L > reach) {
+      s.a = (double)c.G * (double)(reach + DIV::ITEM);
+      s.step = 0;
+    }
+  }
   return s;
 }
 // The numbers of sequence b (one a lane) as they are in memory, and the sequence.
@@ -265,6 +275,33 @@ struct Rows {
   bool ok;
   int pos_first, pos_last;   // of the first and the last row, the same in all lanes
 };
+// With a window, beside that: the first key of it (its position may lie beyond the keys that there are, and this with it).
+struct FarEdge {
+  int from;
+  int from_first, from_last;
+};
+// (of the sequence's first new token; far below zero it hides nothing either way)
+__device__ __forceinline__ int first_from(const PagedCall& c, const Sequence& s) { return (int)max((int64_t)s.base - c.window + 1, -((int64_t)1 << 30)); }
+__device__ __forceinline__ FarEdge far_edge_of(const PagedCall& c, const Sequence& s, int row0, int r) {
+  const int base = first_from(c, s);
+  FarEdge f;
+  f.from = base + token_of(c, min(row0 + r, s.rows - 1));
+  f.from_first = __builtin_amdgcn_readfirstlane(base + token_of(c, min(row0, s.rows - 1)));
+  f.from_last = __builtin_amdgcn_readfirstlane(base + token_of(c, min(row0 + 31, s.rows - 1)));
+  return f;
+}
+// Keys of a tile of 32 NB from k0 on that lie in front of the row's window and are no sinks.
+template <int NB> __device__ __forceinline__ void hide_far(const PagedCall& c, const FarEdge& f, f32x16 (&st)[NB], int k0, int g) {
+  if (k0 < f.from_last && k0 + 32 * NB > c.sinks) {
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = k0 + 32 * kb + 8 * (i >> 2) + 4 * g + (i & 3);
+        if (key < f.from && key >= c.sinks) st[kb][i] = -INFINITY;
+      }
+  }
+}
 __device__ __forceinline__ Rows rows_of(const PagedCall& c, const Sequence& s, int h, int row0, int r) {
   Rows w;
   w.ok = row0 + r < s.rows;
@@ -284,6 +321,34 @@ template <int BR> __device__ __forceinline__ int tiles_of(const PagedCall& c, co
   const int last_row = min((t + 1) * BR, s.rows) - 1;
   const int last = c.causal ? min(s.base + token_of(c, last_row), s.L - 1) : s.L - 1;
   return last < 0 ? 0 : last / keys + 1;
+}
+// The tiles that block t sees, numbered from 0: those of the sinks, then those from the first that its first row's window reaches to that of its last row's position.
+struct SeenTiles {
+  int sink_tiles, first, count;
+  int from;   // the first key of the first row's window
+  // Sixteen rows of a page from `row` on that hold no key that any row of the block sees: their page may belong to another sequence by now, and zeros stand for them.
+  __device__ __forceinline__ bool hidden(const PagedCall& c, int row) const { return row >= c.sinks && row + 16 <= from; }
+  __device__ __forceinline__ int operator()(int i) const { return i < sink_tiles ? i : i - sink_tiles + first; }
+};
+template <int BR> __device__ __forceinline__ SeenTiles seen_tiles(const PagedCall& c, const Sequence& s, int t, int keys) {
+  const int end = tiles_of<BR>(c, s, t, keys);
+  const int from = max(first_from(c, s) + token_of(c, t * BR), 0);
+  SeenTiles m;
+  m.from = __builtin_amdgcn_readfirstlane(from);
+  m.first = __builtin_amdgcn_readfirstlane(from / keys);
+  m.sink_tiles = __builtin_amdgcn_readfirstlane(min((c.sinks + keys - 1) / keys, min(m.first, end)));
+  m.count = __builtin_amdgcn_readfirstlane(m.sink_tiles + max(end - m.first, 0));
+  return m;
+}
+// Without a window: all tiles up to that of the last row's position.
+struct AllTiles {
+  int count;
+  __device__ __forceinline__ bool hidden(const PagedCall&, int) const { return false; }
+  __device__ __forceinline__ int operator()(int i) const { return i; }
+};
+template <bool WINDOW, int BR> __device__ __forceinline__ auto item_tiles(const PagedCall& c, const Sequence& s, int t, int keys) {
+  if constexpr (WINDOW) return seen_tiles<BR>(c, s, t, keys);
+  else return AllTiles{tiles_of<BR>(c, s, t, keys)};
 }
 // Where a cut at distance z of an item of length v falls among its tiles (the same for the pieces on both sides).
 __device__ __forceinline__ int cut_at(double z, double v, int tiles) { return __builtin_amdgcn_readfirstlane(z >= v ? tiles : min(tiles, (int)(z / v * tiles))); }

@@ -34,6 +34,7 @@ struct NormLibrary {
   decltype(&attn_paged_norm_append) append = nullptr;
 };
 NormLibrary norm_lib;
+decltype(&attn_paged_window_fwd) window_fwd = nullptr;
 
 void expect_args(Py_ssize_t n, Py_ssize_t want) {
   if (n != want || lib.rotary == nullptr) raise(PyExc_TypeError, "internal call with the wrong arguments, or before attach_paged()");
@@ -568,16 +569,19 @@ PyObject* append(PyObject* const* a, Py_ssize_t n, bool normed) {
 PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return append(a, n, false); }
 PyObject* py_norm_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return append(a, n, true); }
 
-// paged_fwd(Q, k_cache, v_cache, block_table, lengths, query_starts, softmax_scale, causal, out, lse, workspace) -> (O, LSE)
-PyObject* py_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+// paged_fwd(Q, k_cache, v_cache, block_table, lengths, query_starts, softmax_scale, causal, out, lse, workspace[, window, sinks]) -> (O, LSE)
+PyObject* forward(PyObject* const* a, Py_ssize_t n, bool windowed) {
   return guarded([&]() -> PyObject* {
-    expect_args(n, 11);
+    expect_args(n, windowed ? 13 : 11);
+    const int32_t window = windowed ? clamped32(a[11]) : 0, sinks = windowed ? clamped32(a[12]) : 0;
+    if (windowed && (window < 1 || sinks < 0)) raise(PyExc_ValueError, "window must be at least 1, and sinks must not be negative");
     const at::Tensor& q = tensor(a[0]);
     const Batch b = batch_of(a + 1);
     attn_paged_params p = params_of(q, b);
     p.Hq = narrow(q.size(1));
     p.softmax_scale = (float)number(a[6]);
     p.causal = truth(a[7]);
+    if (windowed && !p.causal) raise(PyExc_ValueError, "a window needs the causal mask");
     at::Tensor out = maybe(a[8]), lse = maybe(a[9]), ws = maybe(a[10]);
     if (out.defined()) {
       expect_like(out, q, "out");
@@ -594,11 +598,15 @@ PyObject* py_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.q_stride_t = axis_stride(q, 0); p.q_stride_h = axis_stride(q, 1); p.o_stride_t = axis_stride(out, 0); p.o_stride_h = axis_stride(out, 1);
     if (!ws.defined()) ws = at::empty({(int64_t)std::max<size_t>(lib.workspace_bytes(&p), 256)}, q.options().dtype(at::kByte));
     check_status(without_gil([&] {
-      return lib.fwd(&p, q.data_ptr(), b.kc.data_ptr(), b.vc.data_ptr(), out.data_ptr(), (float*)lse.data_ptr(), ws.data_ptr(), (size_t)ws.numel() * ws.element_size());
-    }), "attn_paged_fwd");
+      const size_t bytes = (size_t)ws.numel() * ws.element_size();
+      return windowed ? window_fwd(&p, window, sinks, q.data_ptr(), b.kc.data_ptr(), b.vc.data_ptr(), out.data_ptr(), (float*)lse.data_ptr(), ws.data_ptr(), bytes)
+                      : lib.fwd(&p, q.data_ptr(), b.kc.data_ptr(), b.vc.data_ptr(), out.data_ptr(), (float*)lse.data_ptr(), ws.data_ptr(), bytes);
+    }), windowed ? "attn_paged_window_fwd" : "attn_paged_fwd");
     return tuple({a[8] != Py_None ? Py_NewRef(a[8]) : wrap(out), a[9] != Py_None ? Py_NewRef(a[9]) : wrap(lse)});
   });
 }
+PyObject* py_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) { return forward(a, n, false); }
+PyObject* py_window_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) { return forward(a, n, true); }
 
 // paged_workspace_bytes(Q, k_cache, sequences) -> bytes; 0: the sizes are refused
 PyObject* py_workspace_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -662,6 +670,15 @@ PyObject* py_attach(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// attach_paged_window(address of attn_paged_window_fwd)
+PyObject* py_attach_window(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 1) raise(PyExc_TypeError, "attach_paged_window() takes one address");
+    window_fwd = (decltype(window_fwd))low64(a[0]);
+    Py_RETURN_NONE;
+  });
+}
+
 // attach_norm(addresses of attn_norm_rotary, attn_norm_rotary_bwd_workspace_bytes, attn_norm_rotary_bwd, attn_paged_norm_append)
 PyObject* py_attach_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
@@ -701,6 +718,8 @@ void marshal::refuse_eager_graphs(std::initializer_list<const at::Tensor*> tenso
 }
 
 PyMethodDef marshal::paged_methods[] = {
+    {"attach_paged_window", (PyCFunction)(void*)py_attach_window, METH_FASTCALL, nullptr},
+    {"paged_window_fwd", (PyCFunction)(void*)py_window_fwd, METH_FASTCALL, nullptr},
     {"attach_norm", (PyCFunction)(void*)py_attach_norm, METH_FASTCALL, nullptr},
     {"norm_rotary", (PyCFunction)(void*)py_norm_rotary, METH_FASTCALL, nullptr},
     {"norm_rotary_bwd", (PyCFunction)(void*)py_norm_rotary_bwd, METH_FASTCALL, nullptr},

@@ -15,8 +15,8 @@ namespace {
 
 // (cuts moved by up to 48 keys or 64 instead of 32: single tokens of mixed lengths 1 and 3 per cent slower.  SPREAD, us with the join, 0 | 1 | 4 | 16: one token on 30000, 4 heads of 64, 30.0 | 20.5 |
 // 19.8 | 26.1, on 4000 10.6 | 10.6 | 11.0 | 14.1, 8 heads of 128 15.7 | 15.4 | 17.0 | 20.2; two on 10^5 and 64 of 128 to 8192 the same with all four.)
-typedef Division<32, 32, 64, 32, 1> Div;
-constexpr int BR = Div::BR;
+template <bool WINDOW> using DivOf = Division<32, 32, 64, 32, 1, WINDOW>;
+constexpr int BR = DivOf<false>::BR;
 
 // (us, the main kernel.  d = 64, tiles of 64 keys | 32: one token over 777 keys 9.5 | 7.6, 32 sequences of up to 2000 35.9 | 35.1 with the join.  d = 128, 64 sequences and two contexts of
 // 10^5 tokens: two tiles of 32 keys and five wavefronts to a compute unit 108, 163; three and three 97, 143; four and two 103, 151; two tiles of 64 and two wavefronts 110, 148.)
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(64 * JoinShape<D>::kWaves) void paged_one_join_kern
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, bool WINDOW>
 __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
   typedef typename Vec<T>::x8 T8;
   typedef OneShape<D> Shape;
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
   asm volatile("" ::"v"(tro.off[0][0]), "v"(goff[0]), "v"(goff[COPIES - 1]));
 #endif
 
-  Work<Div> work;
+  Work<DivOf<WINDOW>> work;
   if (!work.begin(c, numbers)) return;
   const Point& at = work.at;
   const Sequence& s = work.s;
@@ -227,10 +227,13 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
     const double length = uniform(s.length(at.t));
     const double z1 = work.up_to(length);
     if (z1 == 0.0) break;
-    const int tiles = tiles_of<BR>(c, s, at.t, KEYS);
+    const auto tile = item_tiles<WINDOW, BR>(c, s, at.t, KEYS);   // (tiles are counted among those that are seen)
+    const int tiles = tile.count;
     const int j0 = cut_at(at.z, length, tiles), j1 = cut_at(z1, length, tiles);
     const int L = s.L;
     const Rows w = rows_of(c, s, at.h, at.t * BR, r);
+    FarEdge far;
+    if constexpr (WINDOW) far = far_edge_of(c, s, at.t * BR, r);
     typedef const __attribute__((address_space(4))) int* ScalarInts;   // (scalar loads)
     const ScalarInts table = (ScalarInts)(uintptr_t)(c.b.table + (int64_t)at.b * c.b.table_stride);
     const T* const Kg = (const T*)c.K + (int64_t)at.h * c.b.sh;
@@ -251,7 +254,7 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
       const uint32_t k_lds = lds_addr(&Ks[buf][0]), v_lds = lds_addr(&Vs[buf][0]);
       bool all = (j + 1) * KEYS <= L;
 #pragma unroll
-      for (int i = 0; i < NP; ++i) all = all && (uint32_t)ids[i] < (uint32_t)c.b.pages;
+      for (int i = 0; i < NP; ++i) all = all && (uint32_t)ids[i] < (uint32_t)c.b.pages && !tile.hidden(c, j * KEYS + 16 * i);
       if (all) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
@@ -271,7 +274,7 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
         for (int p = 0; p < COPIES; ++p) {
           const int id = ids[p / PER_PAGE], row = j * KEYS + p * RPC;
           const uint64_t off = (uint64_t)(uint32_t)id * c.b.page_bytes + (uint32_t)(row & c.b.page_mask) * c.b.row_bytes;
-          const bool there = (uint32_t)id < (uint32_t)c.b.pages && row + lane_row < L;
+          const bool there = (uint32_t)id < (uint32_t)c.b.pages && row + lane_row < L && !tile.hidden(c, j * KEYS + 16 * (p / PER_PAGE));
           const void* const kp = there ? (const void*)((const char*)Kg + off + goff[p]) : (const void*)zero_line;
           const void* const vp = there ? (const void*)((const char*)Vg + off + goff[p]) : (const void*)zero_line;
           if (D != 32 || !((beyond >> p) & 1u)) {
@@ -293,7 +296,7 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
         qf[kk] = *(const T8*)(q_row + 16 * kk + 8 * g);
       }
     }
-    if (j0 < j1) page_numbers(j0);
+    if (j0 < j1) page_numbers(tile(j0));
     wait_async_copies();   // Q (the compiler would wait for its loads, and all copies with them, in the loop)
     f32x16 o[DB];
 #pragma unroll
@@ -309,9 +312,9 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
     for (int j = j0 - (STAGES - 1); j < j1; ++j) {
       const int ahead = j + STAGES - 1;
       if (ahead < j1) {   // into the buffer of tile j - 1, which this wavefront is done with
-        copy_tile(ahead, to);
+        copy_tile(tile(ahead), to);
         to = to + 1 == STAGES ? 0 : to + 1;
-        if (ahead + 1 < j1) page_numbers(ahead + 1);
+        if (ahead + 1 < j1) page_numbers(tile(ahead + 1));
       }
       if (j < j0) continue;
       static_assert(STAGES == 3, "the waits below");
@@ -331,7 +334,8 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
         for (int kb = 0; kb < NB; ++kb)
           st[kb] = mfma32(*(const T8*)(Kt + lds_off<D>(32 * kb + r, 2 * kk + g)), qf[kk], st[kb]);
       T8 pf[2 * NB];
-      softmax_tile<T, DB, NB>(st, o, pf, m_run, l_run, lr_run, cs, j * KEYS, w, L, g);
+      if constexpr (WINDOW) hide_far<NB>(c, far, st, tile(j) * KEYS, g);
+      softmax_tile<T, DB, NB>(st, o, pf, m_run, l_run, lr_run, cs, tile(j) * KEYS, w, L, g);
 #pragma unroll
       for (int cc = 0; cc < 2 * NB; ++cc)
 #pragma unroll
@@ -350,7 +354,8 @@ __global__ __launch_bounds__(64, 2) void paged_one_kernel(const PagedCall c) {
 }
 
 template <typename T, int D> int launch(const PagedCall& c, hipStream_t s) {
-  hipLaunchKernelGGL((paged_one_kernel<T, D>), dim3((c.slots + kXcds - 1) / kXcds * kXcds), dim3(64), 0, s, c);
+  if (c.window > 0) hipLaunchKernelGGL((paged_one_kernel<T, D, true>), dim3((c.slots + kXcds - 1) / kXcds * kXcds), dim3(64), 0, s, c);
+  else hipLaunchKernelGGL((paged_one_kernel<T, D, false>), dim3((c.slots + kXcds - 1) / kXcds * kXcds), dim3(64), 0, s, c);
   const int e = (int)hipGetLastError();
   if (e != 0) return e;
   const int rows = c.b.starts ? BR : std::min(c.G, BR);   // of a block, at most

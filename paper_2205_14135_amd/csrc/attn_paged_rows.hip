@@ -21,21 +21,28 @@ namespace {
 // 195 | 195.  Over 76 batches, 32 of them ragged, the same within 1 per cent at d = 128, 6 to 8 less at d = 64; 25 per cent more or less of either changes nothing.
 // SPREAD, us with the join, 4 | 18 | 72 | 288: d = 64, 4 heads, 128 tokens on 60000 65 | 65 | 62 | 76; d = 128, 8 heads, 8 x 16 on 2000 22 | 22 | 22 | 29, 256 on 60000 237 | 240 | 238 | 241, 2048 on 14336 and
 // 8 x 256 the same with all four: anything between 4 and 72 will do.
-typedef Division<256, 64, 320, 320, 18> PairDiv;    // two groups of four wavefronts
-typedef Division<128, 64, 256, 256, 18> BlockDiv;   // four wavefronts
+template <bool WINDOW> using PairDiv = Division<256, 64, 320, 320, 18, WINDOW>;    // two groups of four wavefronts
+template <bool WINDOW> using BlockDiv = Division<128, 64, 256, 256, 18, WINDOW>;   // four wavefronts
 constexpr int BC = 64;
 
 // The copies of a tile that a wavefront makes: 16 rows, which lie in one page.  Page numbers come sixteen tiles at a time, those of their 16-row groups one a lane.
 // An address is scalar work: two 32-bit products (the host checks that a page, and the step from one to the next, are less than 4 GiB).
-template <typename T, int D> struct RowCopies {
+// WINDOW: tiles are those that are seen (SeenTiles), with a gap behind the sinks' ones.
+template <typename T, int D, bool WINDOW> struct RowCopies {
   static constexpr int CPR = D / 8, RPC = 64 / CPR, COPIES = 16 / RPC;
   const int* table;
   int L, part;             // rows 16 part .. + 15 of a tile
   int window, ids, ids_next;
+  SeenTiles seen;   // WINDOW
   uint32_t goff[COPIES];   // byte offset of this lane's chunk of a copy from the first of the 16 rows
   bool beyond;             // D = 32: that chunk lies beyond the tensors' 16 columns
   __device__ __forceinline__ int numbers(const PagedCall& c, int tile) const {
     return table[min(tile * BC + 16 * (int)(threadIdx.x & 63), L - 1) >> c.b.page_log2];
+  }
+  // the sixteen tiles that are asked for behind those of `window`
+  __device__ __forceinline__ int window_behind() const {
+    if constexpr (WINDOW) return window + 16 < seen.sink_tiles ? window + 16 : max(window + 16, seen.first & ~15);
+    return window + 16;
   }
   __device__ __forceinline__ void init(const PagedCall& c, int b, int length, int part_, int first_tile, int lane) {
     table = c.b.table + (int64_t)b * c.b.table_stride;
@@ -60,13 +67,15 @@ template <typename T, int D> struct RowCopies {
 #if defined(__HIP_DEVICE_COMPILE__)
       asm volatile("" : "+v"(ids));   // (arrived from here on: else every tile waits for what might be its load, and for the copies behind that)
 #endif
-      ids_next = numbers(c, window + 16);
+      ids_next = numbers(c, window_behind());
     }
     const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(ids, 4 * (j & 15) + part);
     const int row = j * BC + 16 * part;
     const uint64_t offset = (uint64_t)id * c.b.page_bytes + (uint32_t)(row & c.b.page_mask) * c.b.row_bytes;
     if (D == 32 && beyond) return;
-    if (__builtin_expect(row + 16 <= L && id < (uint32_t)c.b.pages, 1)) {
+    bool there = id < (uint32_t)c.b.pages;
+    if constexpr (WINDOW) there = there && !seen.hidden(c, row);
+    if (__builtin_expect(row + 16 <= L && there, 1)) {
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_part[n]);
@@ -80,7 +89,7 @@ template <typename T, int D> struct RowCopies {
         const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_part[n]);
 #pragma unroll
         for (int p = 0; p < COPIES; ++p)
-          async_copy_b128(id < (uint32_t)c.b.pages && row + p * RPC + lane_row < L ? (const void*)((const char*)tensor[n] + offset + goff[p]) : (const void*)zero_line,
+          async_copy_b128(there && row + p * RPC + lane_row < L ? (const void*)((const char*)tensor[n] + offset + goff[p]) : (const void*)zero_line,
                           lds + p * 1024);
       }
     }
@@ -176,15 +185,15 @@ __global__ __launch_bounds__(2 * BR) void paged_rows_join_kernel(const PagedCall
   write_rows<T, 32>(slice, s, j.h, j.row0 + 32 * wave, o, m, l, lr, stage[wave], db == 0);
 }
 
-template <typename T, int D>
+template <typename T, int D, bool WINDOW>
 __global__ __launch_bounds__(512) void paged_pair_kernel(const PagedCall c) {
   typedef typename Vec<T>::x8 T8;
-  typedef RowCopies<T, D> Copies;
-  constexpr int BR = PairDiv::BR, KK = D / 16, DB = D / 32;
+  typedef RowCopies<T, D, WINDOW> Copies;
+  constexpr int BR = PairDiv<WINDOW>::BR, KK = D / 16, DB = D / 32;
   __shared__ __attribute__((aligned(16))) T Ks[3][BC * D];
   __shared__ __attribute__((aligned(16))) T Vs[3][BC * D];
 
-  Work<PairDiv> work;
+  Work<PairDiv<WINDOW>> work;
   if (!work.begin(c, Round::numbers(c, 0))) return;
   const Point& at = work.at;
   const Sequence& s = work.s;
@@ -197,13 +206,20 @@ __global__ __launch_bounds__(512) void paged_pair_kernel(const PagedCall c) {
     const double z1 = work.up_to(length);
     if (z1 == 0.0) break;
     const bool whole = at.z == 0.0 && z1 == length;
-    const int tiles = tiles_of<BR>(c, s, at.t, BC);
+    const auto tile = item_tiles<WINDOW, BR>(c, s, at.t, BC);   // (tiles are counted among those that are seen)
+    const int tiles = tile.count;
     const int j0 = cut_at(at.z, length, tiles), J = cut_at(z1, length, tiles) - j0;   // tiles j0 .. j0 + J - 1
     const int L = s.L, row0 = at.t * BR + 32 * wave;
     const bool valid = row0 < s.rows;   // wavefronts past the end only keep the barriers company
     // (a lane number that the compiler does not derive things from ahead of the loop over items)
     const int lane = lane_id_here(), r = lane & 31, g = lane >> 5;
     const Rows w = rows_of(c, s, at.h, row0, r);
+    FarEdge far;
+    if constexpr (WINDOW) far = far_edge_of(c, s, row0, r);
+    auto sees = [&](int k0) {
+      if constexpr (WINDOW) return k0 <= w.pos_last && (k0 + BC > far.from_first || k0 < c.sinks);
+      else return k0 <= w.pos_last;
+    };
 
     f32x16 o[DB];
 #pragma unroll
@@ -216,9 +232,10 @@ __global__ __launch_bounds__(512) void paged_pair_kernel(const PagedCall c) {
     if (J > 0) {
       const T* const Tg = (const T*)(group_b ? c.V : c.K) + (int64_t)at.h * c.b.sh;   // what this group copies
       Copies dma;
-      dma.init(c, at.b, L, wave & 3, j0, lane);
+      dma.init(c, at.b, L, wave & 3, tile(j0), lane);
+      if constexpr (WINDOW) dma.seen = tile;
       const uint32_t ring0 = __builtin_amdgcn_readfirstlane(lds_addr(group_b ? &Vs[0][0] : &Ks[0][0]) + dma.part * Copies::COPIES * 1024);
-      auto copy_tile = [&](int j, int k) { dma.template copy<1>(c, j, {Tg}, {ring0 + k * (BC * D * (uint32_t)sizeof(T))}); };
+      auto copy_tile = [&](int j, int k) { dma.template copy<1>(c, tile(j), {Tg}, {ring0 + k * (BC * D * (uint32_t)sizeof(T))}); };
       T8 qf[KK];
       load_q<T, D>(c, w, g, qf);
       const int pos = w.pos;
@@ -228,7 +245,7 @@ __global__ __launch_bounds__(512) void paged_pair_kernel(const PagedCall c) {
       tro.init();
       f32x16 st[2];
       T8 pf[4];
-      auto active = [&](int i) { return valid && (j0 + i) * BC <= w.pos_last; };
+      auto active = [&](int i) { return valid && sees(tile(j0 + i) * BC); };
 
       constexpr int PF = 4;
       auto k_frag = [&](const T* kbuf, int f) {  // f = 2 * kk + kb
@@ -275,7 +292,7 @@ __global__ __launch_bounds__(512) void paged_pair_kernel(const PagedCall c) {
       };
       copy_tile(j0, 0);
       wait_async_copies();   // (and Q)
-      dma.ids_next = dma.numbers(c, dma.window + 16);
+      dma.ids_next = dma.numbers(c, dma.window_behind());
       if (J > 1) copy_tile(j0 + 1, 1);
       __syncthreads();
       if (group_b) {
@@ -293,7 +310,8 @@ __global__ __launch_bounds__(512) void paged_pair_kernel(const PagedCall c) {
         if (more) copy_tile(j0 + i + 2, prv);
         if (active(i)) {
           const KArgs no_dropout = {};
-          softmax_tile_lane_query<T, DB, true, false, false>(no_dropout, st, o, pf, m_run, l_run, lr_run, calm, ones, cs, (j0 + i) * BC, w.pos_first, pos, L, g, 0);
+          if constexpr (WINDOW) hide_far<2>(c, far, st, tile(j0 + i) * BC, g);
+          softmax_tile_lane_query<T, DB, true, false, false>(no_dropout, st, o, pf, m_run, l_run, lr_run, calm, ones, cs, tile(j0 + i) * BC, w.pos_first, pos, L, g, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
         if (more) wait_async_copies_but<Copies::COPIES>(); else wait_async_copies();
@@ -323,15 +341,15 @@ __global__ __launch_bounds__(512) void paged_pair_kernel(const PagedCall c) {
 
 // The same with four wavefronts of 32 rows to a workgroup, which share tiles of K and V in two buffers: three workgroups to a compute unit, so that one's first tiles, ends and
 // diagonal tiles fall into another's full ones.
-template <typename T, int D>
+template <typename T, int D, bool WINDOW>
 __global__ __launch_bounds__(256, 3) void paged_block_kernel(const PagedCall c) {
   typedef typename Vec<T>::x8 T8;
-  typedef RowCopies<T, D> Copies;
-  constexpr int BR = BlockDiv::BR, KK = D / 16, DB = D / 32;
+  typedef RowCopies<T, D, WINDOW> Copies;
+  constexpr int BR = BlockDiv<WINDOW>::BR, KK = D / 16, DB = D / 32;
   __shared__ __attribute__((aligned(16))) T Ks[2][BC * D];
   __shared__ __attribute__((aligned(16))) T Vs[2][BC * D];
 
-  Work<BlockDiv> work;
+  Work<BlockDiv<WINDOW>> work;
   if (!work.begin(c, Round::numbers(c, 0))) return;
   const Point& at = work.at;
   const Sequence& s = work.s;
@@ -343,13 +361,20 @@ __global__ __launch_bounds__(256, 3) void paged_block_kernel(const PagedCall c) 
     const double z1 = work.up_to(length);
     if (z1 == 0.0) break;
     const bool whole = at.z == 0.0 && z1 == length;
-    const int tiles = tiles_of<BR>(c, s, at.t, BC);
+    const auto tile = item_tiles<WINDOW, BR>(c, s, at.t, BC);   // (tiles are counted among those that are seen)
+    const int tiles = tile.count;
     const int j0 = cut_at(at.z, length, tiles), j1 = cut_at(z1, length, tiles);
     const int L = s.L, row0 = at.t * BR + 32 * wave;
     const bool valid = row0 < s.rows;   // wavefronts past the end copy their part of the tiles
     // (a lane number that the compiler does not derive things from ahead of the loop over items)
     const int lane = lane_id_here(), r = lane & 31, g = lane >> 5;
     const Rows w = rows_of(c, s, at.h, row0, r);
+    FarEdge far;
+    if constexpr (WINDOW) far = far_edge_of(c, s, row0, r);
+    auto sees = [&](int k0) {
+      if constexpr (WINDOW) return k0 <= w.pos_last && (k0 + BC > far.from_first || k0 < c.sinks);
+      else return k0 <= w.pos_last;
+    };
 
     f32x16 o[DB];
 #pragma unroll
@@ -368,12 +393,13 @@ __global__ __launch_bounds__(256, 3) void paged_block_kernel(const PagedCall c) 
         __syncthreads();
       }
       Copies dma;
-      dma.init(c, at.b, L, wave, j0, lane);
+      dma.init(c, at.b, L, wave, tile(j0), lane);
+      if constexpr (WINDOW) dma.seen = tile;
       const uint32_t k_lds = __builtin_amdgcn_readfirstlane(lds_addr(&Ks[0][0]) + wave * Copies::COPIES * 1024);
       const uint32_t v_lds = __builtin_amdgcn_readfirstlane(lds_addr(&Vs[0][0]) + wave * Copies::COPIES * 1024);
       auto copy_tile = [&](int j, int buf) {
         const uint32_t at_buf = buf * (BC * D * (uint32_t)sizeof(T));
-        dma.template copy<2>(c, j, {Kg, Vg}, {k_lds + at_buf, v_lds + at_buf});
+        dma.template copy<2>(c, tile(j), {Kg, Vg}, {k_lds + at_buf, v_lds + at_buf});
       };
       copy_tile(j0, 0);
       T8 qf[KK];
@@ -392,12 +418,12 @@ __global__ __launch_bounds__(256, 3) void paged_block_kernel(const PagedCall c) 
 #endif
       }
       wait_async_copies();   // (and Q)
-      dma.ids_next = dma.numbers(c, dma.window + 16);
+      dma.ids_next = dma.numbers(c, dma.window_behind());
       __syncthreads();
       int buf = 0;
       for (int j = j0; j < j1; ++j) {
-        const int k0 = j * BC;
-        const bool active = valid && k0 <= w.pos_last;
+        const int k0 = tile(j) * BC;
+        const bool active = valid && sees(k0);
         constexpr int PF = 4;   // operand reads run ahead of their MFMA
         f32x16 st[2];
 #pragma unroll
@@ -428,6 +454,7 @@ __global__ __launch_bounds__(256, 3) void paged_block_kernel(const PagedCall c) 
         if (active) {
           T8 pf[4];
           const KArgs no_dropout = {};
+          if constexpr (WINDOW) hide_far<2>(c, far, st, k0, g);
           softmax_tile_lane_query<T, DB, true, false, false>(no_dropout, st, o, pf, m_run, l_run, lr_run, calm, ones, cs, k0, w.pos_first, pos, L, g, 0);
           {
             const T* const Vt = Vs[buf];
@@ -464,20 +491,21 @@ __global__ __launch_bounds__(256, 3) void paged_block_kernel(const PagedCall c) 
   }
 }
 
-template <typename T, int D> int launch(const PagedCall& c, hipStream_t s) {
+template <typename T, int D, bool WINDOW> int launch(const PagedCall& c, hipStream_t s) {
   constexpr int BR = paged_block_rows(D);
-  if constexpr (BR == PairDiv::BR) hipLaunchKernelGGL((paged_pair_kernel<T, D>), dim3(c.slots), dim3(2 * BR), 0, s, c);
-  else hipLaunchKernelGGL((paged_block_kernel<T, D>), dim3(c.slots), dim3(2 * BR), 0, s, c);
+  if constexpr (BR == PairDiv<WINDOW>::BR) hipLaunchKernelGGL((paged_pair_kernel<T, D, WINDOW>), dim3(c.slots), dim3(2 * BR), 0, s, c);
+  else hipLaunchKernelGGL((paged_block_kernel<T, D, WINDOW>), dim3(c.slots), dim3(2 * BR), 0, s, c);
   const int e = (int)hipGetLastError();
   if (e != 0) return e;
   hipLaunchKernelGGL((paged_rows_join_kernel<T, D, BR>), dim3(c.slots - 1, D / 32), dim3(2 * BR), 0, s, c);
   return (int)hipGetLastError();
 }
-template <typename T> int launch_t(const PagedCall& c, hipStream_t s) {
-  if (c.d <= 32) return launch<T, 32>(c, s);
-  if (c.d == 64) return launch<T, 64>(c, s);
-  return launch<T, 128>(c, s);
+template <typename T, bool WINDOW> int launch_d(const PagedCall& c, hipStream_t s) {
+  if (c.d <= 32) return launch<T, 32, WINDOW>(c, s);
+  if (c.d == 64) return launch<T, 64, WINDOW>(c, s);
+  return launch<T, 128, WINDOW>(c, s);
 }
+template <typename T> int launch_t(const PagedCall& c, hipStream_t s) { return c.window > 0 ? launch_d<T, true>(c, s) : launch_d<T, false>(c, s); }
 
 }  // namespace
 

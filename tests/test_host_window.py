@@ -84,3 +84,41 @@ def test_marshalling(lib):
             binding.attn_window_bwd(x, x, x, x, x, torch.zeros(1, 2, 100), window=window, sinks=sinks, softmax_scale=0.1)
     with pytest.raises(ValueError):
         binding.attn_window_fwd(x, x[:, :1], x, window=8, softmax_scale=0.1)
+
+
+def _paged(**kw):
+    p = binding.PagedParams()
+    p.B, p.T, p.Hq, p.Hk, p.d, p.dtype, p.pages, p.page_size, p.table_width, p.softmax_scale, p.causal = 2, 2, 8, 2, 64, 1, 10, 16, 4, 0.125, 1
+    p.page_stride, p.head_stride, p.row_stride, p.table_stride = 2 * 16 * 64, 16 * 64, 64, 4
+    p.q_stride_t = p.o_stride_t = 512
+    p.q_stride_h = p.o_stride_h = 64
+    p.block_table, p.lengths = 0x30000, 0x40000
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+@pytest.mark.parametrize("kw,window,sinks,status", [(dict(causal=0), 8, 0, -13), ({}, 0, 0, -13), ({}, -1, 0, -13), ({}, 8, -1, -13), (dict(B=0), 8, 0, -2), (dict(d=48), 8, 0, -4),
+                                                    (dict(page_size=8), 8, 0, -10), (dict(lengths=None), 8, 0, -1), (dict(softmax_scale=0.0), 8, 0, -6)])
+def test_paged_params(lib, kw, window, sinks, status):
+    assert lib.attn_paged_window_fwd(ctypes.byref(_paged(**kw)), window, sinks, *[PTR] * 5, PTR, 1 << 40) == status
+
+
+def test_paged_pointers(lib):
+    p = _paged()
+    need = lib.attn_paged_workspace_bytes(ctypes.byref(p))
+    for i in range(5):
+        args = [PTR] * 5
+        args[i] = None
+        assert lib.attn_paged_window_fwd(ctypes.byref(p), 8, 1, *args, PTR, need) == -1
+    assert lib.attn_paged_window_fwd(ctypes.byref(p), 8, 1, *[PTR] * 5, PTR, need - 1) == -7
+    assert lib.attn_paged_window_fwd(None, 8, 1, *[PTR] * 5, PTR, need) == -1
+
+
+def test_paged_marshalling(lib):
+    q, c = torch.zeros(2, 8, 64, dtype=torch.bfloat16), torch.zeros(10, 2, 16, 64, dtype=torch.bfloat16)
+    t, n = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    for kw, error in ((dict(window=0), ValueError), (dict(window=-3), ValueError), (dict(window=4, sinks=-1), ValueError), (dict(window=4, causal=False), ValueError),
+                      (dict(sinks=3), ValueError), (dict(window=1.5), TypeError), (dict(window=4), RuntimeError)):
+        with pytest.raises(error):
+            binding.attn_paged_fwd(q, c, c, t, n, softmax_scale=0.1, **kw)
