@@ -55,6 +55,7 @@ class _WindowAttention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_out):
         q, k, v, out, lse = ctx.saved_tensors
         if d_out.shape != q.shape or d_out.stride() != q.stride():
@@ -191,7 +192,7 @@ def flash_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, softma
     if window is not None:
         if _node_in_python():
             return _WindowAttention.apply(q, k, v, float(softmax_scale), float(dropout_p), int(seed or 0), int(offset), key_lengths, window, sinks)
-        return binding._marshal.attention(q, k, v, float(softmax_scale), True, float(dropout_p), int(seed or 0), int(offset), key_lengths, None, window, sinks)
+        return binding._marshal.window_attention(q, k, v, float(softmax_scale), float(dropout_p), int(seed or 0), int(offset), key_lengths, window, sinks)
     if _node_in_python():
         apply = _FlashAttention.apply
     else:

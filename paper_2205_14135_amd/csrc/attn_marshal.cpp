@@ -13,7 +13,13 @@
 // defaults) and raise what the Python marshalling of the measurement entry points raises: ValueError, TypeError, AttnError.
 #include "attn_marshal.h"
 
+#include <c10/core/DeviceGuard.h>
+#include <torch/csrc/autograd/function.h>
+#include <torch/csrc/autograd/functions/utils.h>
+#include <torch/csrc/autograd/saved_variable.h>
+
 #include <algorithm>
+#include <mutex>
 #include <vector>
 
 PyObject* marshal::attn_error = nullptr;
@@ -123,8 +129,6 @@ void expect_args(Py_ssize_t n, Py_ssize_t want) {
 struct Attention {
   attn_params p;            // pointers (stream, key lengths) are set again for each call
   at::Tensor key_lengths, block_mask;
-  Window w;
-  Kind kind() const { return w.window != 0 ? kWindow : (block_mask.defined() ? kSparse : kDense); }
 };
 
 attn_params on_current_stream(const Attention& a, const at::Tensor& q) {
@@ -153,21 +157,21 @@ void check_saved(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, 
 }
 
 using torch::autograd::AutogradContext;
+using torch::autograd::SavedVariable;
 using torch::autograd::variable_list;
 
 struct FlashAttention : torch::autograd::Function<FlashAttention> {
   static at::Tensor forward(AutogradContext* ctx, const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, const Attention& a) {
-    const Kind kind = a.kind();
+    const bool sparse = a.block_mask.defined();
     const attn_params p = on_current_stream(a, q);
     const at::Tensor out = like(q, q.scalar_type()), lse = at::empty(q.sizes().slice(0, 3), q.options().dtype(at::kFloat));
     const void *qp = q.data_ptr(), *kp = k.data_ptr(), *vp = v.data_ptr();
     void* op = out.data_ptr();
     float* lp = (float*)lse.data_ptr();
     check_status(without_gil([&] {
-      if (kind == kWindow) return window_lib.fwd(&p, a.w.window, a.w.sinks, qp, kp, vp, op, lp);
-      return kind == kSparse ? lib.sparse_fwd(&p, (const uint8_t*)a.block_mask.data_ptr(), 128, mask_stride(a.block_mask), qp, kp, vp, op, lp)
-                             : lib.fwd(&p, qp, kp, vp, op, lp);
-    }), kForwardNames[kind]);
+      return sparse ? lib.sparse_fwd(&p, (const uint8_t*)a.block_mask.data_ptr(), 128, mask_stride(a.block_mask), qp, kp, vp, op, lp)
+                    : lib.fwd(&p, qp, kp, vp, op, lp);
+    }), sparse ? "attn_blocksparse_fwd" : "attn_fwd");
     ctx->save_for_backward({q, k, v, out, lse});
     auto& data = ctx->saved_data;
     data["softmax_scale"] = (double)a.p.softmax_scale;
@@ -176,11 +180,7 @@ struct FlashAttention : torch::autograd::Function<FlashAttention> {
     data["seed"] = (int64_t)a.p.seed;
     data["offset"] = (int64_t)a.p.offset;
     if (a.key_lengths.defined()) data["key_lengths"] = a.key_lengths;
-    if (kind == kSparse) data["block_mask"] = a.block_mask;
-    if (kind == kWindow) {
-      data["window"] = (int64_t)a.w.window;
-      data["sinks"] = (int64_t)a.w.sinks;
-    }
+    if (sparse) data["block_mask"] = a.block_mask;
     return out;
   }
 
@@ -194,7 +194,6 @@ struct FlashAttention : torch::autograd::Function<FlashAttention> {
     Attention a = {};
     if (data.count("key_lengths")) a.key_lengths = data["key_lengths"].toTensor();
     if (data.count("block_mask")) a.block_mask = data["block_mask"].toTensor();
-    if (data.count("window")) a.w = {(int32_t)data["window"].toInt(), (int32_t)data["sinks"].toInt()};
     check_saved(q, k, v, d_out, a);
     a.p.B = (int32_t)q.size(0); a.p.H = (int32_t)q.size(1); a.p.N = (int32_t)q.size(2); a.p.d = (int32_t)q.size(3);
     a.p.dtype = q.scalar_type() == at::kHalf ? ATTN_FP16 : ATTN_BF16;
@@ -203,29 +202,113 @@ struct FlashAttention : torch::autograd::Function<FlashAttention> {
     a.p.dropout_p = (float)data["dropout_p"].toDouble();
     a.p.seed = (uint64_t)data["seed"].toInt();
     a.p.offset = (uint64_t)data["offset"].toInt();
-    const Kind kind = a.kind();
+    const bool sparse = a.block_mask.defined();
     const attn_params p = on_current_stream(a, q);
     at::Tensor g[3];
     for (at::Tensor& t : g) t = like(q, q.scalar_type());
-    const size_t need = kind == kWindow ? window_lib.workspace_bytes(&p, a.w.window, a.w.sinks) : (kind == kSparse ? lib.sparse_workspace_bytes(&p) : lib.workspace_bytes(&p));
+    const size_t need = sparse ? lib.sparse_workspace_bytes(&p) : lib.workspace_bytes(&p);
     const at::Tensor ws = at::empty({(int64_t)std::max<size_t>(need, 256)}, q.options().dtype(at::kByte));
     const float* lp = (const float*)lse.data_ptr();
     const int status =
-        kind == kWindow ? window_lib.bwd(&p, a.w.window, a.w.sinks, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), d_out.data_ptr(), lp, g[0].data_ptr(), g[1].data_ptr(),
-                                         g[2].data_ptr(), ws.data_ptr(), ws.numel())
-        : kind == kSparse ? lib.sparse_bwd(&p, (const uint8_t*)a.block_mask.data_ptr(), 128, mask_stride(a.block_mask), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        sparse ? lib.sparse_bwd(&p, (const uint8_t*)a.block_mask.data_ptr(), 128, mask_stride(a.block_mask), q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                 out.data_ptr(), d_out.data_ptr(), lp, g[0].data_ptr(), g[1].data_ptr(), g[2].data_ptr(), ws.data_ptr(), ws.numel())
                : lib.bwd(&p, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), d_out.data_ptr(), lp, g[0].data_ptr(), g[1].data_ptr(),
                          g[2].data_ptr(), ws.data_ptr(), ws.numel());
-    if (status != ATTN_OK) refused_in_backward([&] { check_status(status, kBackwardNames[kind]); });
+    if (status != ATTN_OK) refused_in_backward([&] { check_status(status, sparse ? "attn_blocksparse_bwd" : "attn_bwd"); });
     return {g[0], g[1], g[2], at::Tensor()};
   }
 };
 
-// attention(Q, K, V, softmax_scale, causal, dropout_p, seed, offset, key_lengths, block_mask[, window, sinks]) -> O, differentiable
+// Attention with a sliding window: a node of its own class, whose fields are members (a torch::autograd::Function keeps them in a dictionary by name).
+struct WindowAttentionBackward : torch::autograd::Node {
+  SavedVariable q, k, v, out, lse, key_lengths;
+  attn_params p = {};   // strides and pointers are set again for each call
+  Window w = {};
+
+  variable_list apply(variable_list&& grads) override {
+    at::Tensor t[5];
+    Attention a = {};
+    {
+      // (another thread may run the same graph, and its engine let go of the saved tensors)
+      const std::lock_guard<std::mutex> lock(mutex_);
+      t[0] = q.unpack();
+      t[1] = k.unpack();
+      t[2] = v.unpack();
+      t[3] = out.unpack(shared_from_this());
+      t[4] = lse.unpack();
+      a.key_lengths = key_lengths.unpack();
+    }
+    variable_list g(3);
+    if (!grads[0].defined()) return g;
+    // (hooks of the program may have handed back something else than what was saved)
+    const at::Tensor& x = t[0];
+    at::Tensor d_out = grads[0];
+    if (x.sizes() == d_out.sizes() && x.strides() != d_out.strides()) d_out = like(x, x.scalar_type()).copy_(d_out);   // the library addresses dO with the strides of q
+    check_saved(x, t[1], t[2], d_out, a);
+    if (x.size(0) != p.B || x.size(1) != p.H || x.size(2) != p.N || x.size(3) != p.d || (x.scalar_type() == at::kHalf ? ATTN_FP16 : ATTN_BF16) != p.dtype || !alike(x, t[3]) ||
+        t[3].scalar_type() != x.scalar_type() || t[1].scalar_type() != x.scalar_type() || t[2].scalar_type() != x.scalar_type() || d_out.scalar_type() != x.scalar_type() ||
+        t[4].scalar_type() != at::kFloat || t[4].numel() != x.size(0) * x.size(1) * x.size(2) || !t[4].is_contiguous() || t[4].device() != x.device() ||
+        (a.key_lengths.defined() && (a.key_lengths.scalar_type() != at::kInt || a.key_lengths.dim() != 1 || !a.key_lengths.is_contiguous() || a.key_lengths.device() != x.device())))
+      refused_in_backward([] { raise(PyExc_ValueError, "the saved tensors are not those of the forward call"); });
+    const c10::DeviceGuard guard(x.device());
+    a.p = p;
+    const attn_params now = on_current_stream(a, x);
+    for (at::Tensor& y : g) y = like(x, x.scalar_type());
+    const at::Tensor ws = at::empty({(int64_t)std::max<size_t>(window_lib.workspace_bytes(&now, w.window, w.sinks), 256)}, x.options().dtype(at::kByte));
+    const int status = window_lib.bwd(&now, w.window, w.sinks, x.data_ptr(), t[1].data_ptr(), t[2].data_ptr(), t[3].data_ptr(), d_out.data_ptr(), (const float*)t[4].data_ptr(),
+                                      g[0].data_ptr(), g[1].data_ptr(), g[2].data_ptr(), ws.data_ptr(), ws.numel());
+    if (status != ATTN_OK) refused_in_backward([&] { check_status(status, "attn_window_bwd"); });
+    mark_once_differentiable(*this, g, "the gradients of attention with a window cannot be differentiated again");
+    return g;
+  }
+  void release_variables() override {
+    const std::lock_guard<std::mutex> lock(mutex_);
+    for (SavedVariable* s : {&q, &k, &v, &out, &lse, &key_lengths}) s->reset_data();
+  }
+  std::string name() const override { return "WindowAttentionBackward"; }
+};
+
+// window_attention(Q, K, V, softmax_scale, dropout_p, seed, offset, key_lengths, window, sinks) -> O, differentiable
+PyObject* py_window_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    expect_args(n, 10);
+    const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]);
+    same_layout(q, k);
+    same_layout(q, v);
+    Attention at = {};
+    at.p = make_params(a[0], {a[3], Py_True, a[4], a[5], a[6], Py_False, Py_None, a[7]});
+    if (a[7] != Py_None) at.key_lengths = tensor(a[7]);
+    const Window w = window_args(a + 8);
+    if (at::GradMode::is_enabled()) refuse_eager_graphs({&q, &k, &v});
+    const c10::DeviceGuard guard(q.device());
+    const at::Tensor lse = at::empty(q.sizes().slice(0, 3), q.options().dtype(at::kFloat));
+    at::Tensor out = like(q, q.scalar_type());
+    const void *qp = q.data_ptr(), *kp = k.data_ptr(), *vp = v.data_ptr();
+    void* op = out.data_ptr();
+    float* lp = (float*)lse.data_ptr();
+    const attn_params p = on_current_stream(at, q);
+    check_status(without_gil([&] { return window_lib.fwd(&p, w.window, w.sinks, qp, kp, vp, op, lp); }), "attn_window_fwd");
+    if (torch::autograd::compute_requires_grad(q, k, v)) {
+      const std::shared_ptr<WindowAttentionBackward> node(new WindowAttentionBackward(), torch::autograd::deleteNode);
+      node->set_next_edges(torch::autograd::collect_next_edges(q, k, v));
+      node->q = SavedVariable(q, false);
+      node->k = SavedVariable(k, false);
+      node->v = SavedVariable(v, false);
+      node->lse = SavedVariable(lse, false);
+      node->key_lengths = SavedVariable(at.key_lengths, false);
+      node->p = at.p;
+      node->w = w;
+      torch::autograd::set_history(out, node);
+      node->out = SavedVariable(out, true);
+    }
+    return wrap(out);
+  });
+}
+
+// attention(Q, K, V, softmax_scale, causal, dropout_p, seed, offset, key_lengths, block_mask) -> O, differentiable
 PyObject* py_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    expect_args(n, n == 12 ? 12 : 10);
+    expect_args(n, 10);
     const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]);
     same_layout(q, k);
     same_layout(q, v);
@@ -243,11 +326,6 @@ PyObject* py_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       }
       Py_DECREF(block);
       at.block_mask = tensor(a[9]);
-    }
-    if (n == 12) {
-      at.w = window_args(a + 10);
-      if (at.block_mask.defined()) raise(PyExc_ValueError, "a window and a block mask do not go together");
-      if (at::GradMode::is_enabled()) refuse_eager_graphs({&q, &k, &v});
     }
     return wrap(FlashAttention::apply(q, k, v, at));
   });
@@ -364,6 +442,7 @@ PyObject* py_attach_window(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 const PyMethodDef own_methods[] = {
     {"attach_window", (PyCFunction)(void*)py_attach_window, METH_FASTCALL, nullptr},
+    {"window_attention", (PyCFunction)(void*)py_window_attention, METH_FASTCALL, nullptr},
     {"window_fwd", (PyCFunction)(void*)py_window_fwd, METH_FASTCALL, nullptr},
     {"window_bwd", (PyCFunction)(void*)py_window_bwd, METH_FASTCALL, nullptr},
     {"attach", (PyCFunction)(void*)py_attach, METH_FASTCALL, nullptr},

@@ -119,6 +119,9 @@ template <typename F> [[noreturn]] void refused_in_backward(F&& set) {
 // Of a forward pass under capture (attn_paged_marshal.cpp).
 void refuse_eager_graphs(std::initializer_list<const at::Tensor*> tensors);
 
+// Where the gradients of a node are themselves recorded (create_graph): to differentiate them again is an error, whichever of the node's inputs is asked for.
+void mark_once_differentiable(const torch::autograd::Node& node, torch::autograd::variable_list& grads, const char* text);
+
 // The functions of attn_paged_marshal.cpp, ended by an empty entry.
 extern PyMethodDef paged_methods[];
 

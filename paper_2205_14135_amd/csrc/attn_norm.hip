@@ -24,8 +24,31 @@ __device__ __forceinline__ float row_sum(float v, int units_log2) {
   return v;
 }
 
-__device__ __forceinline__ float weight_at(const void* w, bool fp32, int col, _Float16) { return fp32 ? ((const float*)w)[col] : (float)((const _Float16*)w)[col]; }
-__device__ __forceinline__ float weight_at(const void* w, bool fp32, int col, __bf16) { return fp32 ? ((const float*)w)[col] : (float)((const __bf16*)w)[col]; }
+// Eight weights from column `col` (a multiple of 8) on.
+template <typename T> __device__ __forceinline__ void weights_at(const void* w, bool fp32, int col, float* out) {
+  typedef typename Vec<T>::x8 T8;
+  if (fp32) {
+    const float* const p = (const float*)w + col;
+    if (((uintptr_t)w & 15u) == 0) {
+      const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { out[e] = a[e]; out[4 + e] = b[e]; }
+    } else {   // (a part of a longer vector)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) out[e] = p[e];
+    }
+  } else {
+    const T* const p = (const T*)w + col;
+    if (((uintptr_t)w & 15u) == 0) {
+      const T8 a = *(const T8*)p;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) out[e] = (float)a[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) out[e] = (float)p[e];
+    }
+  }
+}
 
 // One unit of one token, as a row of it passes through: 16 values in 32 bits, 8 from column lo on and 8 from hi on.
 template <typename T, Pairing P> struct NormUnit {
@@ -34,11 +57,11 @@ template <typename T, Pairing P> struct NormUnit {
   float w[16], wp[P == kHalvesAny ? 16 : 1];   // wp: of the partner columns
 
   __device__ __forceinline__ void weights(const void* p, bool fp32) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) w[e] = weight_at(p, fp32, e < 8 ? turn.lo + e : turn.hi + e - 8, T());
+    weights_at<T>(p, fp32, turn.lo, w);
+    weights_at<T>(p, fp32, turn.hi, w + 8);
     if constexpr (P == kHalvesAny) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) wp[e] = weight_at(p, fp32, turn.partner[e], T());
+      for (int e = 0; e < 16; ++e) wp[e] = fp32 ? ((const float*)p)[turn.partner[e]] : (float)((const T*)p)[turn.partner[e]];
     }
   }
   static __device__ __forceinline__ void widen(const T8& a, const T8& b, float (&v)[16]) {
@@ -185,7 +208,7 @@ __global__ __launch_bounds__(NT) void norm_append_kernel(const AppendCall c, con
 struct NormItems { int blocks[2]; int64_t items[2]; int groups[2], per[2]; };   // groups: of heads
 
 template <typename T, Pairing P>
-__global__ __launch_bounds__(NT) void norm_rotary_bwd_kernel(const NormBwdCall c, const NormItems w, const int units_log2) {
+__global__ __launch_bounds__(NT, P == kHalvesAny ? 2 : 3) void norm_rotary_bwd_kernel(const NormBwdCall c, const NormItems w, const int units_log2) {
   typedef typename Vec<T>::x8 T8;
   const int i = (int)blockIdx.x < w.blocks[0] ? 0 : 1;
   const int block = (int)blockIdx.x - (i == 0 ? 0 : w.blocks[0]);
@@ -210,67 +233,65 @@ __global__ __launch_bounds__(NT) void norm_rotary_bwd_kernel(const NormBwdCall c
     const T* const x = (const T*)t.x + b * t.xb + n * t.xn;
     const T* const g = (const T*)t.dy + b * t.gb + n * t.gn;
     T* const y = (T*)t.dx + b * t.yb + n * t.yn;
-    constexpr int N = 2;
-    for (int h = h0; h < h1; h += N) {
-      T8 xa[N], xb[N], ga[N], gb[N];
+    // one row is worked on while the next one is on its way
+    auto load = [&](int h, T8 (&v)[4]) {
+      v[0] = *(const T8*)(x + h * t.xh + unit.turn.lo);
+      v[1] = *(const T8*)(x + h * t.xh + unit.turn.hi);
+      v[2] = *(const T8*)(g + h * t.gh + unit.turn.lo);
+      v[3] = *(const T8*)(g + h * t.gh + unit.turn.hi);
+    };
+    T8 next[4];
+    load(h0, next);
+    for (int h = h0; h < h1; ++h) {
+      T8 now[4] = {next[0], next[1], next[2], next[3]};
+      if (h + 1 < h1) load(h + 1, next);
+      float v[16], gv[16], other[P == kHalvesAny ? 16 : 1] = {}, ss = 0.f, hx = 0.f;
+      unit.widen(now[0], now[1], v);
+      unit.widen(now[2], now[3], gv);
+      if constexpr (P == kHalvesAny) {
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        const int64_t hk = min(h + k, h1 - 1);
-        xa[k] = *(const T8*)(x + hk * t.xh + unit.turn.lo);
-        xb[k] = *(const T8*)(x + hk * t.xh + unit.turn.hi);
-        ga[k] = *(const T8*)(g + hk * t.gh + unit.turn.lo);
-        gb[k] = *(const T8*)(g + hk * t.gh + unit.turn.hi);
+        for (int e = 0; e < 16; ++e) other[e] = (float)g[h * t.gh + unit.turn.partner[e]];
       }
+      unit.apply(gv, other);
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        if (h + k >= h1) break;
-        float v[16], gv[16], other[P == kHalvesAny ? 16 : 1] = {}, ss = 0.f, hx = 0.f;
-        unit.widen(xa[k], xb[k], v);
-        unit.widen(ga[k], gb[k], gv);
-        if constexpr (P == kHalvesAny) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) other[e] = (float)g[(h + k) * t.gh + unit.turn.partner[e]];
-        }
-        unit.apply(gv, other);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          ss += v[e] * v[e];
-          hx += gv[e] * unit.w[e] * v[e];
-        }
-        const float r = 1.f / sqrtf(row_sum(ss, units_log2) * inv_d + c.norm.eps);
-        const float back = row_sum(hx, units_log2) * inv_d * r * r;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          dw[e] += gv[e] * v[e] * r;
-          gv[e] = r * (gv[e] * unit.w[e] - v[e] * back);
-        }
-        unit.narrow(gv, ga[k], gb[k]);
-        *(T8*)(y + (h + k) * t.yh + unit.turn.lo) = ga[k];
-        *(T8*)(y + (h + k) * t.yh + unit.turn.hi) = gb[k];
+      for (int e = 0; e < 16; ++e) {
+        ss += v[e] * v[e];
+        hx += gv[e] * unit.w[e] * v[e];
       }
+      const float r = 1.f / sqrtf(row_sum(ss, units_log2) * inv_d + c.norm.eps);
+      const float back = row_sum(hx, units_log2) * inv_d * r * r;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        dw[e] += gv[e] * v[e] * r;
+        gv[e] = r * (gv[e] * unit.w[e] - v[e] * back);
+      }
+      unit.narrow(gv, now[0], now[1]);
+      *(T8*)(y + h * t.yh + unit.turn.lo) = now[0];
+      *(T8*)(y + h * t.yh + unit.turn.hi) = now[1];
     }
   }
   if (t.dw == nullptr) return;
-  // the workgroup's sum: lanes of the same columns, then the wavefronts
-  __shared__ float sums[NT / 64][8][16];
+  // the workgroup's sum: thread rows of 16 columns in LDS, then NT / d (or so) threads a column
+  __shared__ __attribute__((aligned(16))) float sums[NT * 16];
 #pragma unroll
-  for (int e = 0; e < 16; ++e)
-    for (int s = units; s < 64; s <<= 1) dw[e] += __shfl_xor(dw[e], s, 64);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (lane < units) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) sums[wave][u][e] = dw[e];
+  for (int e4 = 0; e4 < 4; ++e4) {
+    const f32x4 v = {dw[4 * e4], dw[4 * e4 + 1], dw[4 * e4 + 2], dw[4 * e4 + 3]};
+    *(f32x4*)(sums + 16 * (int)threadIdx.x + 4 * e4) = v;
   }
   __syncthreads();
-  if ((int)threadIdx.x < units) {
-    float* const out = c.partial + (int64_t)blockIdx.x * c.d;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float s = 0.f;
-#pragma unroll
-      for (int k = 0; k < NT / 64; ++k) s += sums[k][u][e];
-      out[e < 8 ? unit.turn.lo + e : unit.turn.hi + e - 8] = s;
-    }
+  // column `col` of the d = 16 units that a token's threads have, and every `parts`-th token of the workgroup from `part` on
+  const int d = 16 << units_log2, col = (int)threadIdx.x & (d - 1), part = (int)threadIdx.x >> (4 + units_log2), parts = NT >> (4 + units_log2);
+  float s = 0.f;
+  for (int k = part; k < tokens; k += parts) s += sums[k * d + col];
+  __syncthreads();
+  sums[(int)threadIdx.x] = s;
+  __syncthreads();
+  if ((int)threadIdx.x < d) {
+    for (int k = 1; k < parts; ++k) s += sums[k * d + col];
+    Turn<T, P> owner;
+    owner.columns(c.rot, col >> 4);
+    const int e = col & 15;
+    c.partial[(int64_t)blockIdx.x * c.d + (e < 8 ? owner.lo + e : owner.hi + e - 8)] = s;
   }
 }
 

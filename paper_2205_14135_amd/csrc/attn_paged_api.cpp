@@ -221,7 +221,9 @@ int attn_norm_rotary_bwd(const attn_rotary_params* p, const attn_norm_spec* norm
   for (int i = 0; i < n_tensors; ++i)
     for (int j = 0; j < n_tensors; ++j)
       if (c.t[i].dx == c.t[j].x || c.t[i].dx == c.t[j].dy || (i != j && (c.t[i].dx == c.t[j].dx || (c.t[i].dw != nullptr && c.t[i].dw == c.t[j].dw)))) return ATTN_ERR_SHAPE;
-  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < attn::norm_workspace_bytes(p->d)) return ATTN_ERR_WORKSPACE;
+  if ((c.t[0].dw != nullptr || c.t[1].dw != nullptr) &&
+      (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < attn::norm_workspace_bytes(p->d)))
+    return ATTN_ERR_WORKSPACE;
   c.n_tensors = n_tensors;
   c.B = p->B; c.N = p->N; c.d = p->d;
   c.positions = p->positions;

@@ -314,7 +314,7 @@ int norm_gradients(const std::vector<Grad>& g, double eps, const Rotation& r, co
             axis_stride(y, 0), axis_stride(y, 1), axis_stride(y, 2), axis_stride(d, 0), axis_stride(d, 1), axis_stride(d, 2)};
   }
   const attn_norm_spec s = {ptr(g[0].w), g.size() > 1 ? ptr(g[1].w) : nullptr, g[0].w.scalar_type() == at::kFloat, (float)eps};
-  return norm_lib.bwd(&p, &s, t, (int)g.size(), ws.data_ptr(), (size_t)ws.numel() * ws.element_size());
+  return norm_lib.bwd(&p, &s, t, (int)g.size(), const_cast<void*>(ptr(ws)), ws.defined() ? (size_t)ws.numel() * ws.element_size() : 0);
 }
 at::Tensor norm_workspace(const at::Tensor& x) {
   return at::empty({(int64_t)std::max<size_t>(norm_lib.workspace_bytes(narrow(x.size(3))), 256)}, x.options().dtype(at::kByte));
@@ -411,19 +411,15 @@ struct NormRotaryBackward : torch::autograd::Node {
     }
     if (g.empty()) return out;
     const c10::DeviceGuard guard(g[0].x.device());
-    const int status = norm_gradients(g, eps, r, norm_workspace(g[0].x));
+    bool weights = false;
+    for (const Grad& t : g) weights = weights || t.dw.defined();
+    const int status = norm_gradients(g, eps, r, weights ? norm_workspace(g[0].x) : at::Tensor());
     if (status != ATTN_OK) refused_in_backward([&] { check_status(status, "attn_norm_rotary_bwd"); });
     for (size_t n = 0; n < g.size(); ++n) {
       if (should_compute_output(which[n])) out[which[n]] = g[n].dx;
       out[2 + which[n]] = g[n].dw;
     }
-    if (at::GradMode::is_enabled()) {   // the gradients have no gradients: to differentiate them again is an error, whichever of the inputs is asked for
-      torch::autograd::edge_list edges = next_edges();
-      const std::shared_ptr<torch::autograd::Node> error(
-          new torch::autograd::Error("the gradients of norm_rotary_embedding cannot be differentiated again", std::move(edges)), torch::autograd::deleteNode);
-      for (at::Tensor& t : out)
-        if (t.defined()) torch::autograd::set_history(t, error);
-    }
+    mark_once_differentiable(*this, out, "the gradients of norm_rotary_embedding cannot be differentiated again");
     return out;
   }
   void release_variables() override {
@@ -715,6 +711,14 @@ void marshal::refuse_eager_graphs(std::initializer_list<const at::Tensor*> tenso
       raise(PyExc_RuntimeError, "captured while a graph made on the default stream still leads to the same leaf: drop that graph (its outputs) first, or make it on another stream");
     for (const torch::autograd::Edge& e : node->next_edges()) todo.push_back(e.function);
   }
+}
+
+void marshal::mark_once_differentiable(const torch::autograd::Node& node, variable_list& grads, const char* text) {
+  if (!at::GradMode::is_enabled()) return;
+  torch::autograd::edge_list edges = node.next_edges();
+  const std::shared_ptr<torch::autograd::Node> error(new torch::autograd::Error(text, std::move(edges)), torch::autograd::deleteNode);
+  for (at::Tensor& g : grads)
+    if (g.defined()) torch::autograd::set_history(g, error);
 }
 
 PyMethodDef marshal::paged_methods[] = {

@@ -28,8 +28,7 @@ inline void window_plan(WindowArgs& a, int d) {
   a.segment_tiles = 0;
   if (a.sink_blocks == 0) return;
   const int64_t tiles = ((int64_t)a.k.N + qt - 1) / qt, heads = (int64_t)a.k.B * a.k.H;
-  const int64_t own = (a.window + 128 + qt - 1) / qt;
-  const int64_t least = own * 2 < 16 ? 16 : own * 2;
+  const int64_t least = 32;
   int64_t n = (tiles + least - 1) / least;
   const int64_t most = 8 * kComputeUnits / (heads * a.sink_blocks) + 1;
   if (n > most) n = most;

@@ -201,6 +201,39 @@ def test_autograd():
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_hooks_changed_inputs_and_second_gradients():
+    q, k, v, do = _inputs(1, 2, 200, 64, "bf16", 15)
+    leaves = [t.requires_grad_(True) for t in (q, k, v)]
+    run = lambda: flash_attention(*leaves, causal=True, window=50, sinks=2)  # noqa: E731
+    want = torch.autograd.grad(run(), leaves, do)
+    with torch.autograd.graph.save_on_cpu():
+        out = run()
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, leaves, do, retain_graph=True), want))
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, leaves, do), want))
+    with pytest.raises(RuntimeError, match="second time"):
+        torch.autograd.grad(out, leaves, do)
+    for unpack in (lambda x: x[..., :32] if x.dim() == 4 else x, lambda x: x[:, :1] if x.dim() == 3 else x, lambda x: x.half() if x.dim() == 4 else x):
+        with torch.autograd.graph.saved_tensors_hooks(lambda x: x, unpack):
+            out = run()
+        with pytest.raises(ValueError):
+            torch.autograd.grad(out, leaves, do)
+    out = run()
+    with torch.no_grad():
+        v.add_(1)
+    with pytest.raises(RuntimeError, match="inplace"):
+        torch.autograd.grad(out, leaves, do)
+    dq, = torch.autograd.grad(run(), q, do, create_graph=True)
+    for x in leaves:
+        with pytest.raises(RuntimeError, match="cannot be differentiated again"):
+            torch.autograd.grad(dq.float().sum(), x, retain_graph=True)
+    with torch.no_grad():
+        assert run().grad_fn is None
+    # of one input alone
+    x = q.detach().requires_grad_(True)
+    got, = torch.autograd.grad(flash_attention(x, k.detach(), v.detach(), causal=True, window=50, sinks=2), x, do)
+    assert torch.equal(got, torch.autograd.grad(run(), q, do)[0])
+
+
 def test_formula_against_differences():
     """The gradients that the tests compare with, against central differences in 64 bits (h = 2^-16)."""
     gen = torch.Generator().manual_seed(8)
