@@ -113,6 +113,7 @@ struct PagedCall {
   float scale_log2;       // tau * log2(e)
   double longest_line;    // no rising starts make more of the line (attn_paged_line.h) than this
   int window, sinks;      // a token sees the last `window` keys up to its own, and the first `sinks` (window 0: all up to its own)
+  int only;               // with a window: 0 all sequences, 1 those of more than 32 rows, 2 the others
 };
 
 // How attn_paged_fwd runs: blocks of 32 rows, a wavefront each (attn_paged_one.hip), or of 128 or 256 (attn_paged_rows.hip), and the workgroups that share the work.
@@ -129,6 +130,14 @@ constexpr int paged_block_rows(int d) { return d == 128 ? 256 : 128; }
 inline PagedShape paged_shape(int64_t rows, int B, int Hk, int d) {
   if (rows <= (int64_t)32 * B || Hk * ((rows + 31) / 32 + B - 1) < 32) return {32, paged_one_slots(d)};
   return {paged_block_rows(d), paged_rows_slots(d)};
+}
+// With a window: whether sequences of at most 32 rows are worked on in launches of their own, by the kernel for single tokens, behind those of more.  In blocks of 256 rows (d = 128) a tile of one
+// takes nearly as long as of a whole block, and the window, the heads and the batch say how many tiles there may be at most; two launches more are 8 to 12 us.  us, together | apart, 32 / 8 heads
+// of 128, window: 8 single tokens and a chunk of 2048, 4096 214 | 192, 1024 76 | 72; 32 and 2048, 4096 289 | 262; 60 and 4 x 500, 512 83 | 72; two and 2 x 512, 8 / 8 heads, 4096 54 | 62; no single ones, 4 x 512 on 8000,
+// 4096 162 | 167.  d = 64: 32 and a chunk of 1000, 16 / 4 heads, 1024 29 | 44.
+inline bool paged_window_apart(const attn_paged_params& p, const PagedShape& shape, int window, int sinks) {
+  const int64_t reach = (int64_t)window + sinks, capacity = (int64_t)p.table_width * p.page_size;
+  return shape.rows == 256 && (int64_t)p.Hk * (p.B - 1) * (reach < capacity ? reach : capacity) >= 3000 * 64;
 }
 // The number of slots and what to join at each of them (Join in attn_paged_line.h), then two pieces a slot: 32-bit rows of O and three statistics.  Room for either
 // kernel, so that a workspace serves every call at its head dimension.

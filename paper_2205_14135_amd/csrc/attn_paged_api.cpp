@@ -108,6 +108,17 @@ int check_batch_pointers(const attn::PagedBatch& b) {
   return aligned(b.table, 4) && aligned(b.lengths, 4) && aligned(b.starts, 4) ? ATTN_OK : ATTN_ERR_SHAPE;
 }
 
+// The line that the work is laid out on (attn_paged_line.h), at its longest (320: what an item costs beside its keys, at most); false: too long for its arithmetic.
+bool lay_out(const attn_paged_params* p, const attn::PagedShape& shape, attn::PagedCall* out) {
+  attn::PagedCall& c = *out;
+  c.slots = shape.slots;
+  const double rows = (double)p->T * c.G, blocks = rows / shape.rows + p->B;
+  if (p->Hk * (blocks * c.G * ((double)c.b.capacity + 320) + rows * (blocks + 1)) > 0x1p50) return false;
+  // (a sequence of r rows has at most r / BR + 1 blocks, and the sum over these of BR (t + 1) is at most (r + BR) (r / BR + 2) / 2: not above 2^51)
+  c.longest_line = p->Hk * (blocks * c.G * ((double)c.b.capacity + 320) + 0.5 * (rows + (double)p->B * shape.rows) * (rows / shape.rows + 2)) + 1;
+  return true;
+}
+
 // What attn_paged_fwd takes from the params beside the pointers.
 int check_paged(const attn_paged_params* p, attn::PagedCall* out, attn::PagedShape* shape) {
   attn::PagedCall& c = *out;
@@ -125,13 +136,7 @@ int check_paged(const attn_paged_params* p, attn::PagedCall* out, attn::PagedSha
   c.causal = p->causal != 0;
   c.scale_log2 = (float)((double)p->softmax_scale * 1.4426950408889634);
   *shape = attn::paged_shape((int64_t)p->T * c.G, p->B, p->Hk, p->d);
-  c.slots = shape->slots;
-  // the line that the work is laid out on (attn_paged_line.h), at its longest (320: what an item costs beside its keys, at most)
-  const double rows = (double)p->T * c.G, blocks = rows / shape->rows + p->B;
-  if (p->Hk * (blocks * c.G * ((double)c.b.capacity + 320) + rows * (blocks + 1)) > 0x1p50) return ATTN_ERR_SHAPE;
-  // (a sequence of r rows has at most r / BR + 1 blocks, and the sum over these of BR (t + 1) is at most (r + BR) (r / BR + 2) / 2: not above 2^51)
-  c.longest_line = p->Hk * (blocks * c.G * ((double)c.b.capacity + 320) + 0.5 * (rows + (double)p->B * shape->rows) * (rows / shape->rows + 2)) + 1;
-  return ATTN_OK;
+  return lay_out(p, *shape, &c) ? ATTN_OK : ATTN_ERR_SHAPE;
 }
 
 int check_rotary_sizes(const attn_rotary_params* p, int32_t n_tensors) {
@@ -315,6 +320,17 @@ static int paged_fwd(const attn_paged_params* p, int32_t window, int32_t sinks, 
   if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < attn::paged_workspace_bytes(p->d)) return ATTN_ERR_WORKSPACE;
   c.Q = Q; c.K = k_cache; c.V = v_cache; c.O = O; c.LSE = LSE;
   c.part = (float*)workspace;
+  if (window > 0 && attn::paged_window_apart(*p, shape, window, sinks)) {
+    const attn::PagedShape few = {32, attn::paged_one_slots(p->d)};
+    attn::PagedCall single = c;
+    if (lay_out(p, few, &single)) {   // (one after the other, in the same workspace)
+      c.only = 1;
+      single.only = 2;
+      int e = attn::launch_paged_rows(c, p->dtype, (hipStream_t)p->stream);
+      if (e == 0) e = attn::launch_paged_one(single, p->dtype, (hipStream_t)p->stream);
+      return e == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
+    }
+  }
   const int e = shape.rows == 32 ? attn::launch_paged_one(c, p->dtype, (hipStream_t)p->stream) : attn::launch_paged_rows(c, p->dtype, (hipStream_t)p->stream);
   return e == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
 }

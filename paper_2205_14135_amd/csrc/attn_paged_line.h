@@ -37,6 +37,9 @@ template <class DIV> __device__ __forceinline__ Sequence sequence_of(const Paged
   s.base = base;
   s.L = L;
   s.rows = rows;
+  if constexpr (DIV::WINDOW) {
+    if (c.only != 0 && (rows > 32) != (c.only == 1)) s.rows = 0;
+  }
   s.blocks = (s.rows + DIV::BR - 1) / DIV::BR;
   s.a = (double)c.G * ((c.causal ? max(min(base, L), 0) : L) + DIV::ITEM);
   s.step = c.causal ? DIV::BR : 0;

@@ -11,6 +11,7 @@ struct WindowArgs {
   // (window_piece).  The first is of the queries less than a window behind, the others divide those behind them.
   float* part;
   int sink_blocks, segments, segment_tiles;
+  int swept_through;   // != 0: instead, blocks of 128 keys that hold sinks are swept by all queries from the diagonal on, in the one launch (sink_blocks is 0 then)
 };
 
 // Whether the window hides anything at all: if not, the dense causal kernels take the call.
@@ -19,17 +20,23 @@ inline bool window_hides(int N, int window, int sinks) { return (int64_t)window 
 // Rows of a tile of queries in the dK/dV kernels.
 constexpr int window_query_tile(int d) { return d == 128 ? 32 : 64; }
 constexpr size_t window_piece_floats(int d) { return (size_t)2 * 32 * (d <= 32 ? 32 : d); }
-// Blocks of 32 keys that hold sinks, and how the queries at a window's distance and more behind them are divided: stretches of four wavefronts that take as many tiles each as half
-// of those that an ordinary block of keys is swept by, at least 4; fewer stretches where there are many sinks.
+// How the gradients of the sinks are made.  Blocks of keys that hold sinks are swept by the queries behind the window too where that takes no longer than the launch: they come first, two
+// workgroups to a compute unit.  Else those queries are divided in stretches of 32 tiles, eight for each of four wavefronts; fewer, longer ones where there are many sinks.
+// us of the backward pass with four sinks, stretches | swept through, heads x N, window, tiles behind it, tiles of the launch's longest unit: d = 64 16 x 1024, 256, 12 of 2 35.3 | 38.1;
+// 128 x 1024, 256, 12 of 12 88.5 | 80.9; 64 x 2048, 256, 28 of 12 94.2 | 98.0; 128 x 4096, 512, 56 of 80 399 | 394; 16 x 8192, 256, 124 of 12 98 | 240; d = 128 16 x 4096, 1024, 96 of 36 151 | 223;
+// 64 x 4096, 1024, 96 of 144 501 | 486; 64 x 16384, 1024, 480 of 576 2092 | 2054; 1 x 16384, 1024, 480 of 9 163 | 602.
+constexpr int kStretch = 32;
 inline void window_plan(WindowArgs& a, int d) {
   const int qt = window_query_tile(d);
+  a.sink_blocks = a.segments = a.segment_tiles = a.swept_through = 0;
+  if (a.sinks == 0) return;
+  const int64_t tiles = ((int64_t)a.k.N + qt - 1) / qt, heads = (int64_t)a.k.B * a.k.H, behind = tiles - a.window / qt, own = (a.window + 128) / qt;
+  if (behind * 2 * kComputeUnits <= heads * a.k.T * own) {
+    a.swept_through = 1;
+    return;
+  }
   a.sink_blocks = (a.sinks + 31) / 32;
-  a.segments = 0;
-  a.segment_tiles = 0;
-  if (a.sink_blocks == 0) return;
-  const int64_t tiles = ((int64_t)a.k.N + qt - 1) / qt, heads = (int64_t)a.k.B * a.k.H;
-  const int64_t least = 32;
-  int64_t n = (tiles + least - 1) / least;
+  int64_t n = (tiles + kStretch - 1) / kStretch;
   const int64_t most = 8 * kComputeUnits / (heads * a.sink_blocks) + 1;
   if (n > most) n = most;
   a.segment_tiles = (int)((tiles + n - 1) / n);

@@ -30,6 +30,17 @@ struct WindowTiles {
     if (at == sink_end) at = first;
     return t;
   }
+  // The next GROUPS tiles, one for each group of wavefronts; own: that of `group`, -1 past the end.  False once there is none for any.
+  template <int GROUPS> __device__ __forceinline__ bool next_of(int group, int& own) {
+    own = next();
+    const bool any = own >= 0;
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) {
+      const int t = next();
+      if (group == k) own = t;
+    }
+    return any;
+  }
 };
 // Whether rows q0 .. q0 + 31 see any of the tile's keys from k0 on.
 __device__ __forceinline__ bool wave_sees(const WindowArgs& a, int k0, int q0) { return k0 <= q0 + 31 && (q0 - k0 < a.window + TILE - 1 || k0 < a.sinks); }
@@ -47,23 +58,29 @@ __device__ __forceinline__ void hide_far(const WindowArgs& a, f32x16 (&s)[2], in
   }
 }
 
-template <typename T, int D, bool DROPOUT>
-__global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void window_fwd_kernel(const WindowArgs w) {
+// RW wavefronts of 32 rows share the tiles of a workgroup, and KG groups of them work on the same rows, group k on every KG-th tile, in buffers of its own; their (m, l, O) are merged
+// through LDS at the end, as in attn_fwd.hip.
+template <typename T, int D, bool DROPOUT, int RW, int KG>
+__global__ __launch_bounds__(64 * RW * KG, KG == 1 && D <= 64 ? 3 : 2) void window_fwd_kernel(const WindowArgs w) {
   typedef typename Vec<T>::x8 T8;
-  constexpr int KK = D / 16, DB = D / 32, BR = 128, PF = 4;
+  constexpr int KK = D / 16, DB = D / 32, BR = 32 * RW, PF = 4;
   typedef T Tile[TILE * D];
-  __shared__ __attribute__((aligned(16))) Tile Ks[2], Vs[2];
+  __shared__ __attribute__((aligned(16))) Tile bufs[4 * KG];
+  Tile* const Ks = bufs;            // buffers 2 k and 2 k + 1: group k's
+  Tile* const Vs = bufs + 2 * KG;
   const KArgs& a = w.k;
   args_at_once(a);
   const int item = xcd_item(a.n_items, a.chunk);
   if (item < 0) return;
-  const int bh = dealt_head(a, item / a.T), qt = item % a.T;
+  const int n_qt = (a.N + BR - 1) / BR;
+  const int bh = dealt_head(a, item / n_qt), qt = item % n_qt;
   const int b = bh / a.H, h = bh % a.H;
   const int64_t head_off = (int64_t)b * a.sb + (int64_t)h * a.sh;
   const T* __restrict__ Qg = (const T*)a.Q + head_off;
   const T* __restrict__ Kg = (const T*)a.K + head_off;
   const T* __restrict__ Vg = (const T*)a.V + head_off;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / RW;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) - RW * group;
   const int r = lane & 31, g = lane >> 5;
   const int q0 = qt * BR + wave * 32;
   const bool row_ok = q0 + r < a.N;   // (lanes beyond a ragged end work on a copy of the last row and store nothing)
@@ -94,18 +111,18 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void window_fwd_kernel(const 
   it.init<BR>(w, qt * BR, len);
   TrOffsets<D> tro;
   tro.init();
-  TileAsync<T, D, 4> dma;
+  TileAsync<T, D, RW> dma;
   dma.init(a.sn, wave, D == 32 ? a.dvalid : D);
   if (D == 32 && a.dvalid < D) {   // the copies leave columns >= 16 of the tile buffers untouched
-    zero_tiles(&Ks[0][0], 2 * TILE * D);
-    zero_tiles(&Vs[0][0], 2 * TILE * D);
+    zero_tiles(&bufs[0][0], 4 * KG * TILE * D);
     __syncthreads();
   }
   const float c = a.scale_log2;
-  int jt = it.next(), buf = 0;
+  int jt, buf = 0;   // this group's tile, -1 if there is none; more: some group (then the first) has one
+  bool more = it.next_of<KG>(group, jt);
   if (jt >= 0) {
-    dma.copy_rows(Kg, a.sn, jt * TILE, a.N, Ks[0]);
-    dma.copy_rows(Vg, a.sn, jt * TILE, a.N, Vs[0]);
+    dma.copy_rows(Kg, a.sn, jt * TILE, a.N, Ks[2 * group]);
+    dma.copy_rows(Vg, a.sn, jt * TILE, a.N, Vs[2 * group]);
   }
   wait_async_copies();
   __syncthreads();   // the first tile has landed, and so have the Q fragments
@@ -113,18 +130,19 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void window_fwd_kernel(const 
   uint32_t k_off[KK];   // byte offsets of this lane's K fragments in a tile, kept whole
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) {
-    k_off[kk] = lds_addr(&Ks[0][0]) + (uint32_t)(lds_off<D>(r, 2 * kk + g) * sizeof(T));
+    k_off[kk] = lds_addr(&Ks[2 * group][0]) + (uint32_t)(lds_off<D>(r, 2 * kk + g) * sizeof(T));
     asm volatile("" : "+v"(k_off[kk]));
   }
-  while (jt >= 0) {
-    const int jn = it.next();
+  while (KG == 1 ? jt >= 0 : more) {
+    int jn;
+    const bool more_next = it.next_of<KG>(group, jn);
     if (jn >= 0) {   // the next tile streams into the other buffer while this one is used
-      dma.copy_rows(Kg, a.sn, jn * TILE, a.N, Ks[buf ^ 1]);
-      dma.copy_rows(Vg, a.sn, jn * TILE, a.N, Vs[buf ^ 1]);
+      dma.copy_rows(Kg, a.sn, jn * TILE, a.N, Ks[2 * group + (buf ^ 1)]);
+      dma.copy_rows(Vg, a.sn, jn * TILE, a.N, Vs[2 * group + (buf ^ 1)]);
     }
-    const T* Vt = Vs[buf];
+    const T* Vt = Vs[2 * group + buf];
     const int k0 = jt * TILE;
-    if (wave_sees(w, k0, q0)) {
+    if ((KG == 1 || jt >= 0) && wave_sees(w, k0, q0)) {
       f32x16 s[2];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -171,7 +189,45 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void window_fwd_kernel(const 
     wait_async_copies();
     __syncthreads();   // the next tile has landed, and everyone is done with this buffer
     jt = jn;
+    more = more_next;
     buf ^= 1;
+  }
+  if constexpr (KG > 1) {
+    // (the loop ended on a barrier) the groups but the first leave O in the tile buffers from the first one on; the last two take the output rows
+    constexpr int kLanes = 64 * RW;
+    static_assert((KG - 1) * RW + 2 <= 4 * KG && RW <= 4 && sizeof(Tile) == 4 * D * 32, "LDS holds the groups' O and the output rows");
+    __shared__ float sums[(KG - 1) * 3 * kLanes];   // references and row sums
+    f32x4* const o_part = (f32x4*)Ks + (group - 1) * (4 * DB * kLanes) + wave * 64 + lane;
+    float* const s_part = sums + (group - 1) * 3 * kLanes + wave * 64 + lane;
+    if (group > 0) {
+#pragma unroll
+      for (int f = 0; f < 4 * DB; ++f) {
+        const int i = 4 * (f % 4);
+        const f32x4 v = {o[f / 4][i], o[f / 4][i + 1], o[f / 4][i + 2], o[f / 4][i + 3]};
+        o_part[f * kLanes] = v;
+      }
+      s_part[0] = m_run;
+      s_part[kLanes] = l_run;
+      s_part[2 * kLanes] = lr_run[0];
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int k = 1; k < KG; ++k) {
+      const float* const sp = s_part + k * 3 * kLanes;
+      const f32x4* const op = o_part + k * (4 * DB * kLanes);
+      const float mk = sp[0], m = fmaxf(m_run, mk), ref = m == -INFINITY ? 0.f : m;
+      const float w0 = __builtin_amdgcn_exp2f(m_run - ref), w1 = __builtin_amdgcn_exp2f(mk - ref);
+      m_run = m;
+      l_run = l_run * w0 + sp[kLanes] * w1;
+      lr_run[0] = lr_run[0] * w0 + sp[2 * kLanes] * w1;
+#pragma unroll
+      for (int f = 0; f < 4 * DB; ++f) {
+        const f32x4 v = op[f * kLanes];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[f / 4][4 * (f % 4) + e] = o[f / 4][4 * (f % 4) + e] * w0 + v[e] * w1;
+      }
+    }
   }
 
   const float l_sum = l_run + xchg32(l_run);
@@ -194,28 +250,31 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void window_fwd_kernel(const 
         }
     }
   } else {   // through the (now idle) tile buffers
-    T* stage = wave < 2 ? &Ks[0][0] + wave * 32 * D : &Vs[0][0] + (wave - 2) * 32 * D;
+    T* stage = KG > 1 ? &Vs[2 * KG - 2][0] + wave * 32 * D : &bufs[0][0] + wave * 32 * D;
     store_rows_coalesced<T, D>(stage, (T*)a.O + head_off + (int64_t)q0 * a.sn, a.sn, o, inv, a.N - q0, D == 32 ? a.dvalid : D);
   }
 }
 
 // dQ, and -D and the row statistic in base 2 for the dK/dV kernels, as in attn_bwd.hip.
-template <typename T, int D, bool DROPOUT>
-__global__ __launch_bounds__(256, 2) void window_dq_kernel(const WindowArgs w) {
+template <typename T, int D, bool DROPOUT, int RW, int KG>
+__global__ __launch_bounds__(64 * RW * KG, 2) void window_dq_kernel(const WindowArgs w) {
   typedef typename Vec<T>::x8 T8;
-  constexpr int KK = D / 16, DB = D / 32, BR = 128, PF = 4;
-  __shared__ __attribute__((aligned(16))) T Ks[2 * TILE * D];
-  __shared__ __attribute__((aligned(16))) T Vs[2 * TILE * D];
+  constexpr int KK = D / 16, DB = D / 32, BR = 32 * RW, PF = 4;
+  __shared__ __attribute__((aligned(16))) T all[KG * 4 * TILE * D];
+  const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / RW;
+  T* const Ks = all + group * 4 * TILE * D;   // K tile of buffer b at b TILE D, V tile at (2 + b) TILE D
+  T* const Vs = Ks + 2 * TILE * D;
   const KArgs& a = w.k;
   args_at_once(a);
   const int item = xcd_item(a.n_items, a.chunk);
   if (item < 0) return;
-  const int bh = dealt_head(a, item / a.T), qt = item % a.T;
+  const int n_qt = a.T * (4 / RW);   // blocks of BR rows, to the end of the last 128-row block: the scratch vectors are written whole
+  const int bh = dealt_head(a, item / n_qt), qt = item % n_qt;
   const int b = bh / a.H, h = bh % a.H;
   const int64_t head_off = (int64_t)b * a.sb + (int64_t)h * a.sh;
   const T* __restrict__ Kg = (const T*)a.K + head_off;
   const T* __restrict__ Vg = (const T*)a.V + head_off;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) - RW * group;
   const int r = lane & 31, g = lane >> 5;
   const int q0 = qt * BR + wave * 32;
   const bool row_ok = q0 + r < a.N;
@@ -247,7 +306,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(const WindowArgs w) {
   const float lse = a.LSE[(int64_t)bh * a.N + qi];
   const float l2 = (lse == -INFINITY || !row_ok) ? INFINITY : lse * 1.4426950408889634f;
   const float neg_d = row_ok ? -(d_part + xchg32(d_part)) : 0.f;   // -D_i
-  if (g == 0) {   // (the scratch is padded to whole blocks: this workgroup writes all of its block)
+  if (g == 0 && group == 0) {   // (the scratch is padded to whole blocks: this workgroup writes all of its block)
     a.Dvec[(int64_t)bh * a.Nr + q0 + r] = neg_d;
     a.L2vec[(int64_t)bh * a.Nr + q0 + r] = l2;
   }
@@ -262,23 +321,24 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(const WindowArgs w) {
   it.init<BR>(w, qt * BR, len);
   TrOffsets<D> tro;
   tro.init();
-  TileAsync<T, D, 4> dma;
+  TileAsync<T, D, RW> dma;
   dma.init(a.sn, wave, D == 32 ? a.dvalid : D);
   if (D == 32 && a.dvalid < D) {
-    zero_tiles(Ks, 2 * TILE * D);
-    zero_tiles(Vs, 2 * TILE * D);
+    zero_tiles(all, KG * 4 * TILE * D);
     __syncthreads();
   }
   const float c = a.scale_log2;
-  int jt = it.next(), buf = 0;
+  int jt, buf = 0;
+  bool more = it.next_of<KG>(group, jt);
   if (jt >= 0) {
     dma.copy_rows(Kg, a.sn, jt * TILE, a.N, Ks);
     dma.copy_rows(Vg, a.sn, jt * TILE, a.N, Vs);
   }
   wait_async_copies();
   __syncthreads();
-  while (jt >= 0) {
-    const int jn = it.next();
+  while (KG == 1 ? jt >= 0 : more) {
+    int jn;
+    const bool more_next = it.next_of<KG>(group, jn);
     if (jn >= 0) {
       dma.copy_rows(Kg, a.sn, jn * TILE, a.N, Ks + (buf ^ 1) * TILE * D);
       dma.copy_rows(Vg, a.sn, jn * TILE, a.N, Vs + (buf ^ 1) * TILE * D);
@@ -286,7 +346,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(const WindowArgs w) {
     const T* Kt = Ks + buf * TILE * D;
     const T* Vt = Vs + buf * TILE * D;
     const int k0 = jt * TILE;
-    if (wave_sees(w, k0, q0)) {
+    if ((KG == 1 || jt >= 0) && wave_sees(w, k0, q0)) {
       f32x16 s[2], dp[2];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -364,29 +424,70 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(const WindowArgs w) {
     wait_async_copies();
     __syncthreads();
     jt = jn;
+    more = more_next;
     buf ^= 1;
   }
-  T* stage = wave < 2 ? Ks + wave * 32 * D : Vs + (wave - 2) * 32 * D;
+  if constexpr (KG > 1) {
+    // (the loop ended on a barrier) the groups but the first leave their dQ in the tile buffers
+    constexpr int kLanes = 64 * RW;
+    static_assert((KG - 1) * DB * 16 * kLanes * 4 <= KG * 4 * TILE * D * (int)sizeof(T), "LDS holds the groups' dQ");
+    f32x4* const part = (f32x4*)all + wave * 64 + lane;
+    if (group > 0) {
+#pragma unroll
+      for (int f = 0; f < 4 * DB; ++f) {
+        const int i = 4 * (f % 4);
+        const f32x4 v = {dq[f / 4][i], dq[f / 4][i + 1], dq[f / 4][i + 2], dq[f / 4][i + 3]};
+        part[((group - 1) * 4 * DB + f) * kLanes] = v;
+      }
+    }
+    __syncthreads();
+    if (group == 0) {
+#pragma unroll
+      for (int k = 0; k < KG - 1; ++k)
+#pragma unroll
+        for (int f = 0; f < 4 * DB; ++f) {
+          const f32x4 v = part[(k * 4 * DB + f) * kLanes];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dq[f / 4][4 * (f % 4) + e] += v[e];
+        }
+    }
+    __syncthreads();   // the buffers stage the output rows
+    if (group > 0) return;
+  }
+  T* stage = all + wave * 32 * D;
   store_rows_coalesced<T, D>(stage, (T*)a.dQ + head_off + (int64_t)q0 * a.sn, a.sn, dq, a.tau, a.N - q0, D == 32 ? a.dvalid : D);
 }
 
-void set_items(KArgs& k, int blocks) {
-  k.n_items = k.B * k.H * blocks;
-  k.chunk = (k.n_items + kXcds - 1) / kXcds;
+// The division of the forward and of dQ among wavefronts: with few blocks of rows, half as many rows to a block and two groups of wavefronts that take every other tile.
+// us, {4, 1} | {2, 2} (wavefronts of rows, groups), heads x N, window: forward d = 64 12 x 197, 64 7.2 | 5.1, 16 x 1024, 256 11.1 | 8.0, 8 x 4096, 512 15.8 | 12.9, 32 x 1024, 256 11.5 | 10.1,
+// 48 x 1024, 256 15.1 | 15.7, 16 x 4096, 512 21.1 | 23.4; d = 128 1 x 16384, 1024 28.7 | 22.6, 16 x 1024, 256 13.9 | 11.7, 32 x 1024, 256 14.8 | 22.0; d = 32 60 x 1000, 300 14.4 | 11.8.
+// Backward (dQ alone so): d = 64 8 x 4096, 512 35.2 | 33.3, 32 x 1024, 256 27.4 | 26.8, 48 x 1024, 256 35.9 | 38.9; d = 128 1 x 16384, 1024 142 | 134, 4 x 8192, 1024 112 | 122; d = 32 30 x 1000, 300
+// 23.5 | 20.9, 60 x 1000, 300 30.2 | 31.7.
+bool window_divided(const WindowArgs& a, int64_t compute_units_blocks) {
+  const int64_t blocks64 = (int64_t)a.k.B * a.k.H * ((a.k.N + 63) / 64);
+  return blocks64 <= compute_units_blocks * kComputeUnits;
 }
-template <typename T, int D> int launch_fwd(WindowArgs a, bool dropout, hipStream_t s) {
-  set_items(a.k, a.k.T);
-  const dim3 grid(kXcds * a.k.chunk), block(256);
-  if (dropout) hipLaunchKernelGGL((window_fwd_kernel<T, D, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((window_fwd_kernel<T, D, false>), grid, block, 0, s, a);
+template <typename T, int D, int RW, int KG> int launch_fwd(WindowArgs a, bool dropout, hipStream_t s) {
+  a.k.n_items = a.k.B * a.k.H * ((a.k.N + 32 * RW - 1) / (32 * RW));
+  a.k.chunk = (a.k.n_items + kXcds - 1) / kXcds;
+  const dim3 grid(kXcds * a.k.chunk), block(64 * RW * KG);
+  if (dropout) hipLaunchKernelGGL((window_fwd_kernel<T, D, true, RW, KG>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((window_fwd_kernel<T, D, false, RW, KG>), grid, block, 0, s, a);
   return (int)hipGetLastError();
 }
-template <typename T, int D> int launch_dq(WindowArgs a, bool dropout, hipStream_t s) {
-  set_items(a.k, a.k.T);
-  const dim3 grid(kXcds * a.k.chunk), block(256);
-  if (dropout) hipLaunchKernelGGL((window_dq_kernel<T, D, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((window_dq_kernel<T, D, false>), grid, block, 0, s, a);
+template <typename T, int D, int RW, int KG> int launch_dq(WindowArgs a, bool dropout, hipStream_t s) {
+  a.k.n_items = a.k.B * a.k.H * a.k.T * (4 / RW);
+  a.k.chunk = (a.k.n_items + kXcds - 1) / kXcds;
+  const dim3 grid(kXcds * a.k.chunk), block(64 * RW * KG);
+  if (dropout) hipLaunchKernelGGL((window_dq_kernel<T, D, true, RW, KG>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((window_dq_kernel<T, D, false, RW, KG>), grid, block, 0, s, a);
   return (int)hipGetLastError();
+}
+template <typename T, int D> int launch_fwd(const WindowArgs& a, bool dropout, hipStream_t s) {
+  return window_divided(a, D == 128 ? 1 : (D == 64 ? 2 : 4)) ? launch_fwd<T, D, 2, 2>(a, dropout, s) : launch_fwd<T, D, 4, 1>(a, dropout, s);
+}
+template <typename T, int D> int launch_dq(const WindowArgs& a, bool dropout, hipStream_t s) {
+  return window_divided(a, D == 128 ? 1 : 2) ? launch_dq<T, D, 2, 2>(a, dropout, s) : launch_dq<T, D, 4, 1>(a, dropout, s);
 }
 
 }  // namespace

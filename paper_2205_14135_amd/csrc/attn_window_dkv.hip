@@ -1,6 +1,7 @@
 // dK and dV of attention with a sliding window and first tokens that stay visible, gfx950.
 //
-// Arithmetic and register layout are those of attn_bwd_dkv_fr128.hip (lane = key; one wavefront does all four tile products of its 32 keys).  The pairs of a query and a key fall in two:
+// Arithmetic and register layout are those of attn_bwd_dkv_fr128.hip (lane = key; one wavefront does all four tile products of its 32 keys). 
+// With few queries behind the window the blocks of keys that hold sinks are swept by those too (WindowArgs::swept_through).  Else the pairs of a query and a key fall in two:
 //   window_dkv_kernel   pairs less than a window apart.  A block of 128 keys is swept by the (window + 128) / QT tiles of queries from the diagonal on, whatever the length.
 //   window_sinks_kernel pairs of a sink and a query a window or more behind it.  There are few such keys and many such queries: a workgroup takes 32 keys and a stretch of the
 // queries, its four wavefronts every fourth tile of it, in buffers of their own.
@@ -43,17 +44,20 @@ __global__ __launch_bounds__(256, SINKS ? 1 : 2) void window_dkv_kernel(const Wi
   KeepLK keep;
   if constexpr (DROPOUT) keep.init(keep_table, a.drop_thr);
 
-  const int item = xcd_item(a.n_items, a.chunk);
-  if (item < 0) return;
-  // SINKS: item = (head, block of 32 keys, stretch), else (head, block of 128 keys)
+  // SINKS: item = (head, block of 32 keys, stretch).  Else the heads are dealt round the XCDs, and the blocks of an XCD's heads come in their order, the first of all of them first: they
+  // may be swept through, and neighbours read the same queries.
   int bh, kt, segment = 0;
   if constexpr (SINKS) {
+    const int item = xcd_item(a.n_items, a.chunk);
+    if (item < 0) return;
     segment = item % w.segments;
     kt = item / w.segments % w.sink_blocks;
     bh = dealt_head(a, item / w.segments / w.sink_blocks);
   } else {
-    kt = item % a.T;
-    bh = dealt_head(a, item / a.T);
+    const int place = (int)blockIdx.x / kXcds, heads = a.chunk;   // heads of an XCD, rounded up
+    kt = place / heads;
+    bh = place % heads * kXcds + (int)blockIdx.x % kXcds;
+    if (bh >= a.B * a.H) return;
   }
   const int b = bh / a.H, h = bh % a.H;
   const int64_t head_off = (int64_t)b * a.sb + (int64_t)h * a.sh;
@@ -94,8 +98,9 @@ __global__ __launch_bounds__(256, SINKS ? 1 : 2) void window_dkv_kernel(const Wi
     limit = min(limit, (segment + 1) * w.segment_tiles);
   } else {
     first = kb0 / QT;
-    limit = min((int64_t)limit, ((int64_t)kb0 + BR - 1 + w.window - 1) / QT + 1);
+    if (!(w.swept_through && kb0 < w.sinks)) limit = min((int64_t)limit, ((int64_t)kb0 + BR - 1 + w.window - 1) / QT + 1);
   }
+  const bool to_the_end = !SINKS && w.swept_through && kw0 < w.sinks;   // of this wavefront's keys
   if (kb0 >= len) limit = 0;
 
   TrOffsets<D> tro;
@@ -136,13 +141,14 @@ __global__ __launch_bounds__(256, SINKS ? 1 : 2) void window_dkv_kernel(const Wi
     first_query = kj < len && kj < w.sinks ? kj + w.window : 0x7fffffff;
     last_query = 0x7fffffff;
   }
+  if (to_the_end && kj < w.sinks) last_query = 0x7fffffff;
   const bool short_of_keys = kw0 + 32 > len || (SINKS && kw0 + 32 > w.sinks);
   auto tile_step = [&](int t, bool has_tile, int t_next, bool has_next, auto buf_c) __attribute__((always_inline)) {
     constexpr int buf = decltype(buf_c)::value;
     if (has_next) fetch_tile(t_next, buf ^ 1);
     const int i0 = t * QT;
     // (rows of the workgroup's tiles that this wavefront's keys have no pair with)
-    if (has_tile && (SINKS || (i0 + QT > kw0 && i0 <= kw0 + 31 + w.window - 1))) {
+    if (has_tile && (SINKS || (i0 + QT > kw0 && (to_the_end || i0 <= kw0 + 31 + w.window - 1)))) {
       const T* Qt = Qs0 + buf * QT * D;
       const T* Gt = Gs0 + buf * QT * D;
       f32x16 s[QB], dp[QB];
@@ -274,7 +280,7 @@ __global__ __launch_bounds__(256, SINKS ? 1 : 2) void window_dkv_kernel(const Wi
     }
     if (group > 0) return;
   }
-  if (SINKS || kw0 < w.sinks) {   // a piece (the same for all lanes: a sink among the 32 keys)
+  if (SINKS || (w.sink_blocks > 0 && kw0 < w.sinks)) {   // a piece (the same for all lanes: a sink among the 32 keys)
     f32x4* const piece = window_piece<D>(w, bh, SINKS ? kt : kw0 / 32, SINKS ? 1 + segment : 0) + lane;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
@@ -333,9 +339,9 @@ __global__ __launch_bounds__(64) void window_join_kernel(const WindowArgs w, con
 template <typename T, int D, bool DROPOUT> int launch(WindowArgs a, hipStream_t s) {
   KArgs& k = a.k;
   const int heads = k.B * k.H;
-  k.n_items = heads * k.T;
-  k.chunk = (k.n_items + kXcds - 1) / kXcds;
-  hipLaunchKernelGGL((window_dkv_kernel<T, D, DROPOUT, false>), dim3(kXcds * k.chunk), dim3(256), 0, s, a);
+  k.chunk = (heads + kXcds - 1) / kXcds;
+  k.n_items = k.chunk * k.T;
+  hipLaunchKernelGGL((window_dkv_kernel<T, D, DROPOUT, false>), dim3(kXcds * k.n_items), dim3(256), 0, s, a);
   int e = (int)hipGetLastError();
   if (e != 0 || a.sink_blocks == 0) return e;
   k.n_items = heads * a.sink_blocks * a.segments;

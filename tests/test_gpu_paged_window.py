@@ -121,6 +121,19 @@ def test_a_chunk_among_single_tokens():
     check(ph.Batch([900, 0, 2000, 31, 64], [1, 300, 1, 1, 1], 8, 2, 64, "bf16", 16, pad=3, seed=5), 150, 4)
 
 
+@pytest.mark.parametrize("new", [[1, 500, 1, 16, 17, 0, 1, 9], [40, 33, 300, 64], [1] * 7 + [900]])
+def test_few_rows_are_worked_on_apart(new):
+    """Long windows, wide tables, d = 128: sequences of at most 32 rows (16 tokens of two heads a group) go to the kernel for single tokens, the others to that for chunks."""
+    B = len(new)
+    batch = ph.Batch([(b * 1237) % 3000 for b in range(B)], new, 32, 16, 128, "bf16", 16, pad=3, seed=30)
+    wide = torch.full((B, 400), -1, dtype=torch.int32)
+    wide[:, :batch.table.shape[1]] = batch.table
+    batch.table = wide
+    assert 16 * (B - 1) * min(6400, 4500) >= 3000 * 64       # (the rule's bound)
+    check(batch, 4500, 0)
+    check(ph.Batch([(b * 1237) % 3000 for b in range(B)], new, 32, 16, 128, "fp16", 256, pad=3, seed=31), 2600, 1900)
+
+
 @pytest.mark.parametrize("new", [[2, 3, 1], [1, 1, 1]])
 def test_few_tokens_with_starts(new):
     check(ph.Batch([600, 20, 2100], new, 8, 2, 128, "bf16", 16, pad=2, seed=6), 250, 3)

@@ -90,6 +90,13 @@ def test_many_heads():
     _check(3, 11, 700, 64, "bf16", 200, 4, lengths=[700, 90, 400], heads=[(0, 0), (1, 3), (2, 10)])
 
 
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("N,window,sinks,kw", [(300, 200, 4, {}), (300, 150, 140, {}), (333, 200, 40, dict(p=0.2)), (300, 200, 5, dict(lengths=[300, 17, 256, 129, 0, 299, 300])), (260, 130, 129, {})])
+def test_sinks_that_are_swept_through(d, N, window, sinks, kw):
+    """Many heads, few tiles behind the window: the blocks of keys that hold sinks take all queries."""
+    _check(7, 30, N, d, "bf16", window, sinks, heads=[(0, 0), (2, 17), (3, 1), (6, 29)], **kw)
+
+
 def test_more_sinks_than_segments_can_share():
     _check(4, 20, 1500, 32, "fp16", 100, 40, heads=[(0, 0), (3, 19)])
 
