@@ -21,24 +21,31 @@ inline bool window_hides(int N, int window, int sinks) { return (int64_t)window 
 constexpr int window_query_tile(int d) { return d == 128 ? 32 : 64; }
 constexpr size_t window_piece_floats(int d) { return (size_t)2 * 32 * (d <= 32 ? 32 : d); }
 // How the gradients of the sinks are made.  Blocks of keys that hold sinks are swept by the queries behind the window too where that takes no longer than the launch: they come first, two
-// workgroups to a compute unit.  Else those queries are divided in stretches of 32 tiles, eight for each of four wavefronts; fewer, longer ones where there are many sinks.
-// us of the backward pass with four sinks, stretches | swept through, heads x N, window, tiles behind it, tiles of the launch's longest unit: d = 64 16 x 1024, 256, 12 of 2 35.3 | 38.1;
-// 128 x 1024, 256, 12 of 12 88.5 | 80.9; 64 x 2048, 256, 28 of 12 94.2 | 98.0; 128 x 4096, 512, 56 of 80 399 | 394; 16 x 8192, 256, 124 of 12 98 | 240; d = 128 16 x 4096, 1024, 96 of 36 151 | 223;
-// 64 x 4096, 1024, 96 of 144 501 | 486; 64 x 16384, 1024, 480 of 576 2092 | 2054; 1 x 16384, 1024, 480 of 9 163 | 602.
-constexpr int kStretch = 32;
+// workgroups to a compute unit.  Else those queries are divided in stretches, which four wavefronts each take the tiles of in turn: about 128 in all, of at least 16 tiles, and of no more than
+// the other blocks of keys leave time for (a stretch's tile takes a quarter of twice as long as theirs).
+// us of the backward pass with four sinks, stretches of 32 tiles | swept through, heads x N, window, tiles behind it, tiles of the launch's longest unit: d = 64 16 x 1024, 256, 12 of 2 25.6 | 38.3;
+// 128 x 1024, 256, 12 of 12 82.0 | 80.2; 64 x 2048, 256, 28 of 12 78.2 | 97.3; 300 x 300, 150, 3 of 7 56.5 | 50.9; d = 128 16 x 4096, 1024, 96 of 36 135 | 223; 210 x 333, 200, 5 of 12 85.8 | 70.6;
+// 64 x 16384, 1024, 480 of 576 2053 | 2040; 1 x 16384, 1024, 480 of 9 154 | 600.  Stretches of 16 | 32 | 64: d = 64 4 x 2048, 128 22.4 | 28.1 | 27.9; d = 32 8 x 8192, 100 28.1 | 30.1 | 39.8,
+// 60 x 3000, 300, 40 sinks 77.1 | 78.8 | 75.8; d = 128 16 x 16384, 1024 553 | 534 | 527.
 inline void window_plan(WindowArgs& a, int d) {
   const int qt = window_query_tile(d);
   a.sink_blocks = a.segments = a.segment_tiles = a.swept_through = 0;
   if (a.sinks == 0) return;
   const int64_t tiles = ((int64_t)a.k.N + qt - 1) / qt, heads = (int64_t)a.k.B * a.k.H, behind = tiles - a.window / qt, own = (a.window + 128) / qt;
+  const int64_t unit = heads * a.k.T * own / (2 * kComputeUnits);   // tiles that a compute unit's two workgroups take one after the other
   if (behind * 2 * kComputeUnits <= heads * a.k.T * own) {
     a.swept_through = 1;
     return;
   }
   a.sink_blocks = (a.sinks + 31) / 32;
-  int64_t n = (tiles + kStretch - 1) / kStretch;
-  const int64_t most = 8 * kComputeUnits / (heads * a.sink_blocks) + 1;
+  int64_t stretch = tiles * heads * a.sink_blocks / 128;
+  if (stretch > 2 * unit && stretch > 64) stretch = 2 * unit > 64 ? 2 * unit : 64;
+  if (stretch < 16) stretch = 16;
+  // (no more pieces than two workgroups a compute unit and one a block: the workspace stays linear in the sinks and the heads)
+  int64_t n = (tiles + stretch / 2) / stretch;
+  const int64_t most = 2 * kComputeUnits / (heads * a.sink_blocks) + 1;
   if (n > most) n = most;
+  if (n < 1) n = 1;
   a.segment_tiles = (int)((tiles + n - 1) / n);
   a.segments = (int)((tiles + a.segment_tiles - 1) / a.segment_tiles);
 }

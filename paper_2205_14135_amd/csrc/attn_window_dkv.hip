@@ -1,12 +1,13 @@
 // dK and dV of attention with a sliding window and first tokens that stay visible, gfx950.
 //
 // Arithmetic and register layout are those of attn_bwd_dkv_fr128.hip (lane = key; one wavefront does all four tile products of its 32 keys). 
-// With few queries behind the window the blocks of keys that hold sinks are swept by those too (WindowArgs::swept_through).  Else the pairs of a query and a key fall in two:
-//   window_dkv_kernel   pairs less than a window apart.  A block of 128 keys is swept by the (window + 128) / QT tiles of queries from the diagonal on, whatever the length.
-//   window_sinks_kernel pairs of a sink and a query a window or more behind it.  There are few such keys and many such queries: a workgroup takes 32 keys and a stretch of the
-// queries, its four wavefronts every fourth tile of it, in buffers of their own.
-// Wavefronts whose 32 keys hold sinks leave dV^T and dK^T of either kernel in the workspace, in 32 bits; window_join_kernel adds the pieces up in their order and rounds once: no atomics,
-// the same bits every time.
+// A block of 128 keys is swept by the (window + 128) / QT tiles of queries from the diagonal on, whatever the length.  What is left are the pairs of a sink and a query a window or more
+// behind it: few keys and many queries.  Either the blocks that hold sinks are swept by all queries (WindowArgs::swept_through), or workgroups in front of the others take 32 keys and a
+// stretch of the queries each, their four wavefronts every fourth tile of it, in buffers of their own (window_plan says which).
+// Then wavefronts whose 32 keys hold sinks leave dV^T and dK^T of either part in the workspace, in 32 bits, and window_join_kernel adds the pieces up in their order and rounds once: no
+// atomics, the same bits every time.
+// (The stretches in a launch of their own: us of the backward pass with four sinks 16 x 1024, window 256, d = 64 35.4 -> 25.6, 16 x 4096, 1024, d = 128 147 -> 131, 16 x 2048, 512 75 -> 58;
+// 16 x 16384, 1024, whose other blocks fill the chip four times exactly, the same.)
 // Vector registers: d = 128 keeps the V rows in LDS (as there) and 32 queries to a tile, d <= 64 both operands in registers and 64 queries.
 #include "attn_window.h"
 
@@ -22,43 +23,38 @@ template <int D> __device__ __forceinline__ f32x4* window_piece(const WindowArgs
   return (f32x4*)(w.part + (((int64_t)bh * w.sink_blocks + block) * (1 + w.segments) + index) * (2 * 32 * D));
 }
 
+// What a workgroup of either kind has in LDS, one block, so that every address is a per-lane register plus an immediate: for each group of wavefronts row statistics and tiles of Q and dO, in
+// BUFS buffers, and at d = 128 the V rows of the keys.
+template <typename T, int D, bool SINKS> struct DkvShape {
+  static constexpr int QT = window_query_tile(D), RW = SINKS ? 1 : 4, KG = SINKS ? 4 : 1, BUFS = SINKS ? 1 : 2, BR = 32 * RW;
+  static constexpr int kVecBytes = 2 * BUFS * 64 * 4, kGroupBytes = kVecBytes + 2 * BUFS * QT * D * (int)sizeof(T);
+  static constexpr int kBytes = KG * kGroupBytes + (D == 128 ? BR * D * (int)sizeof(T) : 0);
+};
+
+// SINKS: a block of 32 keys and a stretch of queries, else a block of 128 keys.  place: of the workgroup among those of its kind.
 template <typename T, int D, bool DROPOUT, bool SINKS>
-__global__ __launch_bounds__(256, SINKS ? 1 : 2) void window_dkv_kernel(const WindowArgs w) {
+__device__ __forceinline__ void window_dkv_block(const WindowArgs& w, unsigned char* const all, uint32_t* const keep_table, const int number) {
   typedef typename Vec<T>::x8 T8;
-  constexpr int KK = D / 16, DB = D / 32, QT = window_query_tile(D), QB = QT / 32;
-  constexpr int RW = SINKS ? 1 : 4, KG = SINKS ? 4 : 1, BR = 32 * RW;
+  typedef DkvShape<T, D, SINKS> Shape;
+  constexpr int KK = D / 16, DB = D / 32, QT = Shape::QT, QB = QT / 32, RW = Shape::RW, KG = Shape::KG, BUFS = Shape::BUFS, BR = Shape::BR;
   constexpr bool V_IN_LDS = D == 128;
-  // One LDS block, so that every address is a per-lane register plus an immediate: the row vectors, the Q tiles, the dO tiles, and the V rows of the keys
-  constexpr int kVecBytes = 4 * 64 * 4, kGroupBytes = kVecBytes + 4 * QT * D * (int)sizeof(T);
-  __shared__ __attribute__((aligned(16))) unsigned char all[KG * kGroupBytes + (V_IN_LDS ? BR * D * (int)sizeof(T) : 0)];
   const KArgs& a = w.k;
   const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wave = KG == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
-  unsigned char* const smem = all + group * kGroupBytes;
+  unsigned char* const smem = all + group * Shape::kGroupBytes;
   float* const Ls0 = (float*)smem;                 // base-2 row statistic, 64 a buffer
-  float* const Ds0 = Ls0 + 2 * 64;                 // -D_i
-  T* const Qs0 = (T*)(smem + kVecBytes);
-  T* const Gs0 = Qs0 + 2 * QT * D;
-  T* const Vb = (T*)(all + KG * kGroupBytes);
-  __shared__ __attribute__((aligned(16))) uint32_t keep_table[DROPOUT ? KeepLK::kTable : 4];
+  float* const Ds0 = Ls0 + BUFS * 64;              // -D_i
+  T* const Qs0 = (T*)(smem + Shape::kVecBytes);
+  T* const Gs0 = Qs0 + BUFS * QT * D;
+  T* const Vb = (T*)(all + KG * Shape::kGroupBytes);
   KeepLK keep;
   if constexpr (DROPOUT) keep.init(keep_table, a.drop_thr);
 
-  // SINKS: item = (head, block of 32 keys, stretch).  Else the heads are dealt round the XCDs, and the blocks of an XCD's heads come in their order, the first of all of them first: they
-  // may be swept through, and neighbours read the same queries.
-  int bh, kt, segment = 0;
-  if constexpr (SINKS) {
-    const int item = xcd_item(a.n_items, a.chunk);
-    if (item < 0) return;
-    segment = item % w.segments;
-    kt = item / w.segments % w.sink_blocks;
-    bh = dealt_head(a, item / w.segments / w.sink_blocks);
-  } else {
-    const int place = (int)blockIdx.x / kXcds, heads = a.chunk;   // heads of an XCD, rounded up
-    kt = place / heads;
-    bh = place % heads * kXcds + (int)blockIdx.x % kXcds;
-    if (bh >= a.B * a.H) return;
-  }
+  // The heads are dealt round the XCDs.  The blocks of an XCD's heads come in their order, the first of all of them first: they may be swept through, and neighbours read the same queries.
+  const int place = number / kXcds, heads = a.chunk;   // heads of an XCD, rounded up
+  const int bh = place % heads * kXcds + number % kXcds;
+  if (bh >= a.B * a.H) return;
+  const int kt = SINKS ? place / heads / w.segments : place / heads, segment = SINKS ? place / heads % w.segments : 0;
   const int b = bh / a.H, h = bh % a.H;
   const int64_t head_off = (int64_t)b * a.sb + (int64_t)h * a.sh;
   const T* __restrict__ Qg = (const T*)a.Q + head_off;
@@ -108,7 +104,7 @@ __global__ __launch_bounds__(256, SINKS ? 1 : 2) void window_dkv_kernel(const Wi
   TileAsync<T, D, RW, QT> dma;
   dma.init(a.sn, wave, D == 32 ? a.dvalid : D);
   if (D == 32 && a.dvalid < D) {   // the copies leave columns >= 16 of the tile buffers untouched
-    zero_tiles((T*)all, KG * kGroupBytes / (int)sizeof(T));
+    zero_tiles((T*)all, KG * Shape::kGroupBytes / (int)sizeof(T));
     __syncthreads();
   }
   auto fetch_tile = [&](int t, int buf) {
@@ -131,7 +127,7 @@ __global__ __launch_bounds__(256, SINKS ? 1 : 2) void window_dkv_kernel(const Wi
       }
     }
   }
-  if (first + group < limit) fetch_tile(first + group, 0);
+  if (!SINKS && first < limit) fetch_tile(first, 0);
   wait_async_copies();
   __syncthreads();
 
@@ -143,12 +139,11 @@ __global__ __launch_bounds__(256, SINKS ? 1 : 2) void window_dkv_kernel(const Wi
   }
   if (to_the_end && kj < w.sinks) last_query = 0x7fffffff;
   const bool short_of_keys = kw0 + 32 > len || (SINKS && kw0 + 32 > w.sinks);
-  auto tile_step = [&](int t, bool has_tile, int t_next, bool has_next, auto buf_c) __attribute__((always_inline)) {
+  auto products = [&](int t, auto buf_c) __attribute__((always_inline)) {
     constexpr int buf = decltype(buf_c)::value;
-    if (has_next) fetch_tile(t_next, buf ^ 1);
     const int i0 = t * QT;
     // (rows of the workgroup's tiles that this wavefront's keys have no pair with)
-    if (has_tile && (SINKS || (i0 + QT > kw0 && (to_the_end || i0 <= kw0 + 31 + w.window - 1)))) {
+    if ((SINKS || (i0 + QT > kw0 && (to_the_end || i0 <= kw0 + 31 + w.window - 1)))) {
       const T* Qt = Qs0 + buf * QT * D;
       const T* Gt = Gs0 + buf * QT * D;
       f32x16 s[QB], dp[QB];
@@ -239,21 +234,32 @@ __global__ __launch_bounds__(256, SINKS ? 1 : 2) void window_dkv_kernel(const Wi
         }
       }
     }
-    wait_async_copies();
-    __syncthreads();
   };
   const std::integral_constant<int, 0> buf0;
   const std::integral_constant<int, 1> buf1;
-  for (int t0 = first; t0 < limit; t0 += 2 * KG) {   // (the same number of steps in every group)
-    const int t = t0 + group;
-    tile_step(t, KG == 1 || t < limit, t + KG, t + KG < limit, buf0);
-    if (t0 + KG < limit) tile_step(t + KG, KG == 1 || t + KG < limit, t + 2 * KG, t + 2 * KG < limit, buf1);
+  if constexpr (SINKS) {   // (buffers of the wavefront's own: no barriers; other workgroups fill its waits)
+    for (int t = first + group; t < limit; t += KG) {
+      fetch_tile(t, 0);
+      wait_async_copies();
+      products(t, buf0);
+    }
+  } else {
+    auto step = [&](int t, auto buf_c) __attribute__((always_inline)) {
+      if (t + 1 < limit) fetch_tile(t + 1, decltype(buf_c)::value ^ 1);
+      products(t, buf_c);
+      wait_async_copies();
+      __syncthreads();
+    };
+    for (int t = first; t < limit; t += 2) {
+      step(t, buf0);
+      if (t + 1 < limit) step(t + 1, buf1);
+    }
   }
 
   if constexpr (SINKS) {
-    // the loop ended on a barrier: the groups but the first leave dV, then dK in the buffers, and the first one adds them up
+    // the groups but the first leave dV, then dK in the buffers, and the first one adds them up
     f32x4* const part = (f32x4*)all + lane;
-    static_assert(3 * 4 * DB * 64 * 16 <= KG * kGroupBytes, "LDS holds one gradient of the groups");
+    static_assert(3 * 4 * DB * 64 * 16 <= Shape::kBytes, "LDS holds one gradient of the groups");
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
       f32x16 (&x)[DB] = which == 0 ? dv : dk;
@@ -296,12 +302,22 @@ __global__ __launch_bounds__(256, SINKS ? 1 : 2) void window_dkv_kernel(const Wi
   }
   if constexpr (!SINKS) {
     // (the loop ended on a barrier: the tile buffers stage the output rows)
-    static_assert(4 * 32 * D * (int)sizeof(T) <= 4 * QT * D * (int)sizeof(T), "room for a gradient's rows");
+    static_assert(4 * 32 * D <= 2 * BUFS * QT * D, "room for a gradient's rows");
     T* const stage = Qs0 + wave * 32 * D;
     store_rows_coalesced<T, D>(stage, (T*)a.dV + head_off + (int64_t)kw0 * a.sn, a.sn, dv, DROPOUT ? a.keep_scale : 1.f, a.N - kw0, D == 32 ? a.dvalid : D);
     __builtin_amdgcn_wave_barrier();
     store_rows_coalesced<T, D>(stage, (T*)a.dK + head_off + (int64_t)kw0 * a.sn, a.sn, dk, a.tau, a.N - kw0, D == 32 ? a.dvalid : D);
   }
+}
+
+// The first `sink_groups` workgroups (a multiple of the XCDs) take the sinks' stretches, so that their waits for memory fall into the others' products.
+template <typename T, int D, bool DROPOUT>
+__global__ __launch_bounds__(256, 2) void window_dkv_kernel(const WindowArgs w, const int sink_groups) {
+  constexpr int kBytes = DkvShape<T, D, true>::kBytes > DkvShape<T, D, false>::kBytes ? DkvShape<T, D, true>::kBytes : DkvShape<T, D, false>::kBytes;
+  __shared__ __attribute__((aligned(16))) unsigned char all[kBytes];
+  __shared__ __attribute__((aligned(16))) uint32_t keep_table[DROPOUT ? KeepLK::kTable : 4];
+  if ((int)blockIdx.x < sink_groups) window_dkv_block<T, D, DROPOUT, true>(w, all, keep_table, (int)blockIdx.x);
+  else window_dkv_block<T, D, DROPOUT, false>(w, all, keep_table, (int)blockIdx.x - sink_groups);
 }
 
 // blockIdx.x: a head's block of 32 keys with sinks; blockIdx.y: 32 columns of dV (the first D / 32) or of dK, a wavefront each.  Four pieces are on their way at a time.  (All columns of
@@ -340,15 +356,10 @@ template <typename T, int D, bool DROPOUT> int launch(WindowArgs a, hipStream_t 
   KArgs& k = a.k;
   const int heads = k.B * k.H;
   k.chunk = (heads + kXcds - 1) / kXcds;
-  k.n_items = k.chunk * k.T;
-  hipLaunchKernelGGL((window_dkv_kernel<T, D, DROPOUT, false>), dim3(kXcds * k.n_items), dim3(256), 0, s, a);
-  int e = (int)hipGetLastError();
+  const int sink_groups = kXcds * k.chunk * a.sink_blocks * a.segments;
+  hipLaunchKernelGGL((window_dkv_kernel<T, D, DROPOUT>), dim3(sink_groups + kXcds * k.chunk * k.T), dim3(256), 0, s, a, sink_groups);
+  const int e = (int)hipGetLastError();
   if (e != 0 || a.sink_blocks == 0) return e;
-  k.n_items = heads * a.sink_blocks * a.segments;
-  k.chunk = (k.n_items + kXcds - 1) / kXcds;
-  hipLaunchKernelGGL((window_dkv_kernel<T, D, DROPOUT, true>), dim3(kXcds * k.chunk), dim3(256), 0, s, a);
-  e = (int)hipGetLastError();
-  if (e != 0) return e;
   hipLaunchKernelGGL((window_join_kernel<T, D>), dim3(heads * a.sink_blocks, 2 * (D / 32)), dim3(64), 0, s, a, DROPOUT ? k.keep_scale : 1.f);
   return (int)hipGetLastError();
 }
