@@ -119,6 +119,23 @@ at::Tensor like(const at::Tensor& q, at::ScalarType type) {
   return at::empty_strided(q.sizes(), q.strides(), q.options().dtype(type));
 }
 
+// What the calls with a window ask of their tensors beside what all calls do: one type, one GPU, and outputs that hold what is written.
+void expect_type(const at::Tensor& q, std::initializer_list<const at::Tensor*> others) {
+  if (!q.is_cuda()) raise(PyExc_RuntimeError, "runs on the GPU only: there is no CPU path");
+  for (const at::Tensor* t : others)
+    if (t->scalar_type() != q.scalar_type()) raise(PyExc_TypeError, "all [B,H,N,d] tensors must have the same type");
+}
+void expect_rows_like(const at::Tensor& q, const at::Tensor& t, bool fp32) {
+  if (!alike(q, t) || t.scalar_type() != (fp32 ? at::kFloat : q.scalar_type())) raise(PyExc_ValueError, "a tensor of rows has another shape, other strides, another type or device than Q");
+}
+void expect_statistic(const at::Tensor& q, const at::Tensor& t) {
+  if (t.scalar_type() != at::kFloat || t.sizes() != q.sizes().slice(0, 3) || !t.is_contiguous() || t.device() != q.device())
+    raise(PyExc_ValueError, "lse must be a contiguous float32 tensor [B,H,N] on the device of Q");
+}
+void expect_lengths(const at::Tensor& q, PyObject* lengths) {   // (their type and shape: make_params)
+  if (lengths != Py_None && tensor(lengths).device() != q.device()) raise(PyExc_ValueError, "all tensors must be on the same device");
+}
+
 void expect_args(Py_ssize_t n, Py_ssize_t want) {
   if (n != want || lib.fwd == nullptr) raise(PyExc_TypeError, "internal call with the wrong arguments, or before attach()");
 }
@@ -279,6 +296,8 @@ PyObject* py_window_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     at.p = make_params(a[0], {a[3], Py_True, a[4], a[5], a[6], Py_False, Py_None, a[7]});
     if (a[7] != Py_None) at.key_lengths = tensor(a[7]);
     const Window w = window_args(a + 8);
+    expect_type(q, {&k, &v});
+    expect_lengths(q, a[7]);
     if (at::GradMode::is_enabled()) refuse_eager_graphs({&q, &k, &v});
     const c10::DeviceGuard guard(q.device());
     const at::Tensor lse = at::empty(q.sizes().slice(0, 3), q.options().dtype(at::kFloat));
@@ -346,6 +365,14 @@ PyObject* forward(PyObject* const* a, Py_ssize_t n, Kind kind) {
     if (kind == kWindow) w = window_args(r + 2);
     const at::Tensor out = r[0] != Py_None ? tensor(r[0]) : like(q, p.o_fp32 ? at::kFloat : q.scalar_type());
     const at::Tensor lse = r[1] != Py_None ? tensor(r[1]) : at::empty(q.sizes().slice(0, 3), q.options().dtype(at::kFloat));
+    c10::OptionalDeviceGuard guard;
+    if (kind == kWindow) {
+      expect_type(q, {&k, &v});
+      expect_rows_like(q, out, p.o_fp32);
+      expect_statistic(q, lse);
+      expect_lengths(q, a[3 + 7]);
+      guard.reset_device(q.device());
+    }
     const void *qp = q.data_ptr(), *kp = k.data_ptr(), *vp = v.data_ptr();
     void* op = out.data_ptr();
     float* lp = (float*)lse.data_ptr();
@@ -378,6 +405,16 @@ PyObject* backward(PyObject* const* a, Py_ssize_t n, Kind kind) {
     for (int i = 0; i < 3; ++i) {
       if (allocate) g[i] = like(q, q.scalar_type());
       gp[i] = allocate ? g[i].data_ptr() : data(r[2 + i]);
+    }
+    c10::OptionalDeviceGuard guard;
+    if (kind == kWindow) {
+      expect_type(q, {&k, &v, &go});
+      expect_rows_like(q, tensor(a[3]), p.o_fp32);
+      expect_statistic(q, tensor(a[5]));
+      expect_lengths(q, a[6 + 7]);
+      for (int i = 0; i < 3 && !allocate; ++i) expect_rows_like(q, tensor(r[2 + i]), false);
+      if (r[0] != Py_None && (!tensor(r[0]).is_contiguous() || tensor(r[0]).device() != q.device())) raise(PyExc_ValueError, "the workspace must be contiguous, on the device of Q");
+      guard.reset_device(q.device());
     }
     at::Tensor ws;
     if (r[0] != Py_None) {

@@ -315,3 +315,27 @@ def test_c_entry_points_refuse_a_short_workspace():
     need = binding.attn_window_bwd_workspace_bytes(binding.make_params(q, 0.1, True), 50, 2)
     with pytest.raises(binding.AttnError):
         binding.attn_window_bwd(q, k, v, O, do, L, window=50, sinks=2, softmax_scale=0.1, workspace=torch.empty(need - 256, dtype=torch.uint8, device="cuda"))
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    q, k, v, do = _inputs(1, 2, 100, 64, "bf16", 21)
+    kw = dict(window=20, softmax_scale=0.1)
+    O, L = binding.attn_window_fwd(q, k, v, **kw)
+    for out, lse, error in ((O[:, :1], L, ValueError), (O.float(), L, ValueError), (O.cpu(), L, ValueError), (O, L[:, :, :50], ValueError), (O, L.double(), ValueError), (O, L.cpu(), ValueError),
+                            (torch.empty(1, 2, 100, 128, dtype=torch.bfloat16, device="cuda")[..., :64], L, ValueError)):
+        with pytest.raises(error):
+            binding.attn_window_fwd(q, k, v, out=out, lse=lse, **kw)
+        with pytest.raises(error):
+            binding.attn_window_bwd(q, k, v, out, do, lse, **kw)
+    with pytest.raises(ValueError):
+        binding.attn_window_fwd(q, k, v, out=O, o_fp32=True, **kw)
+    with pytest.raises(TypeError):
+        binding.attn_window_fwd(q, k.half(), v, **kw)
+    with pytest.raises(TypeError):
+        flash_attention(q, k, v.float(), causal=True, window=20)
+    with pytest.raises(ValueError):
+        binding.attn_window_bwd(q, k, v, O, do, L, grads=(q, k, v[:, :, :50]), **kw)
+    with pytest.raises(ValueError):
+        binding.attn_window_bwd(q, k, v, O, do, L, workspace=torch.empty(1 << 20, dtype=torch.uint8), **kw)
+    with pytest.raises(ValueError):
+        binding.attn_window_fwd(q, k, v, key_lengths=torch.ones(1, dtype=torch.int32), **kw)

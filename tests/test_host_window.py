@@ -84,6 +84,10 @@ def test_marshalling(lib):
             binding.attn_window_bwd(x, x, x, x, x, torch.zeros(1, 2, 100), window=window, sinks=sinks, softmax_scale=0.1)
     with pytest.raises(ValueError):
         binding.attn_window_fwd(x, x[:, :1], x, window=8, softmax_scale=0.1)
+    with pytest.raises(RuntimeError, match="GPU only"):
+        binding.attn_window_fwd(x, x, x, window=8, softmax_scale=0.1)
+    with pytest.raises(RuntimeError, match="GPU only"):
+        binding.attn_window_bwd(x, x, x, x, x, torch.zeros(1, 2, 100), window=8, softmax_scale=0.1)
 
 
 def _paged(**kw):
