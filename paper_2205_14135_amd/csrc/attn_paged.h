@@ -139,6 +139,19 @@ inline bool paged_window_apart(const attn_paged_params& p, const PagedShape& sha
   const int64_t reach = (int64_t)window + sinks, capacity = (int64_t)p.table_width * p.page_size;
   return shape.rows == 256 && (int64_t)p.Hk * (p.B - 1) * (reach < capacity ? reach : capacity) >= 3000 * 64;
 }
+// With a window and one new token a sequence: a workgroup for each block of 32 rows, of as many wavefronts as LDS has room for with three tiles of 32 keys each, in one launch
+// (attn_paged_few.hip).  Where a wavefront has up to 6 tiles, or up to 12 and the workgroups are not so few that most of the device would idle, and up to 512 workgroups: more of them take turns on a
+// compute unit, and a division by keys is evener.  us, divided with the join | this, sequences x K heads (workgroups), window.  d = 64: 1 x 2, 512 (3 tiles) 9.9 | 7.0, 1024 10.1 | 9.9, 2048 (11) 10.8 | 15.2;
+// 64 x 2, 512 14.0 | 7.9, 2048 23.1 | 17.3; 256 x 2, 512 27.6 | 19.3, 2048 59 | 50; 1024 x 2, 512 80 | 67.  d = 128: 1 x 8, 256 (3) 13.7 | 9.9, 512 (6) 13.8 | 13.2, 1024 (11) 14.5 | 21.0; 16 x 8, 256 14.3 |
+// 10.6, 1024 22.4 | 22.3; 33 x 8, 512 26.5 | 27.5; 64 x 8, 256 27.4 | 24.7, 512 35.6 | 33.0; 128 x 8, 512 58 | 62; 256 x 8, 256 71 | 83.  d = 32: 1 x 12, 2048 (8) 11.6 | 12.1; 20 x 12, 512 15.0 | 7.3, 2048 24.4 |
+// 15.3; 200 x 12, 512 48 | 55.
+constexpr int paged_few_waves(int d) { return d <= 32 ? 8 : (d == 64 ? 6 : 3); }
+inline int64_t paged_few_items(const PagedCall& c) { return (int64_t)c.b.B * c.b.Hk * ((c.G + 31) / 32); }
+inline bool paged_few(const PagedCall& c) {
+  if (c.window == 0 || c.b.starts != nullptr) return false;
+  const int64_t items = paged_few_items(c), reach = (int64_t)c.window + c.sinks, keys = reach < c.b.capacity ? reach : c.b.capacity;
+  return items <= 512 && keys <= (int64_t)(items < 64 ? 6 : 12) * 32 * paged_few_waves(c.d);
+}
 // The number of slots and what to join at each of them (Join in attn_paged_line.h), then two pieces a slot: 32-bit rows of O and three statistics.  Room for either
 // kernel, so that a workspace serves every call at its head dimension.
 constexpr int kJoinBytes = 32;
@@ -156,6 +169,7 @@ int launch_norm_rotary(const NormCall& c, int dtype, hipStream_t s);
 int launch_norm_append(const AppendCall& c, const NormArgs& norm, int dtype, hipStream_t s);
 int launch_norm_rotary_bwd(const NormBwdCall& c, int dtype, hipStream_t s);
 int launch_paged_one(const PagedCall& c, int dtype, hipStream_t s);
+int launch_paged_few(const PagedCall& c, int dtype, hipStream_t s);
 int launch_paged_rows(const PagedCall& c, int dtype, hipStream_t s);
 // pairs: host memory, (source, destination) page numbers, checked by the caller; bytes of a row: d * 2.
 struct CopyCall {

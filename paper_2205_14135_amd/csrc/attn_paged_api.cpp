@@ -320,6 +320,7 @@ static int paged_fwd(const attn_paged_params* p, int32_t window, int32_t sinks, 
   if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < attn::paged_workspace_bytes(p->d)) return ATTN_ERR_WORKSPACE;
   c.Q = Q; c.K = k_cache; c.V = v_cache; c.O = O; c.LSE = LSE;
   c.part = (float*)workspace;
+  if (attn::paged_few(c)) return attn::launch_paged_few(c, p->dtype, (hipStream_t)p->stream) == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
   if (window > 0 && attn::paged_window_apart(*p, shape, window, sinks)) {
     const attn::PagedShape few = {32, attn::paged_one_slots(p->d)};
     attn::PagedCall single = c;

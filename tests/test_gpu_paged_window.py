@@ -139,6 +139,20 @@ def test_few_tokens_with_starts(new):
     check(ph.Batch([600, 20, 2100], new, 8, 2, 128, "bf16", 16, pad=2, seed=6), 250, 3)
 
 
+@pytest.mark.parametrize("single", [True, False])
+@pytest.mark.parametrize("d,page,Hq,Hk", [(16, 16, 66, 2), (32, 32, 12, 12), (64, 16, 33, 1), (128, 64, 8, 8)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (31, 33), (95, 1), (577, 0), (1500, 65), (6000, 3)])
+def test_single_tokens_of_mixed_lengths(d, page, Hq, Hk, window, sinks, single):
+    """Without `starts` up to a number of tiles by a workgroup for each, beyond that, and with them, divided."""
+    n = [5, 0, 1, 97, 1600, 32, 0, 6400]
+    check(ph.Batch([x - 1 if single else max(x - 1, 0) for x in n], [1 if single else min(x, 1) for x in n], Hq, Hk, d, "bf16", page, seed=d + window), window, sinks, single=single)
+
+
+@pytest.mark.parametrize("B,Hq,Hk,d", [(63, 1, 1, 64), (64, 1, 1, 64), (128, 4, 4, 16), (171, 3, 3, 32), (129, 4, 4, 128), (9, 33 * 32, 32, 64)])
+def test_either_side_of_a_number_of_workgroups(B, Hq, Hk, d):
+    check(ph.Batch([(37 * i) % 1400 for i in range(B)], [1] * B, Hq, Hk, d, "fp16", 16, seed=B), 1300, 2, single=True)
+
+
 @pytest.mark.parametrize("Hq,d", [(40, 64), (71, 64), (128, 128)])
 def test_many_heads_share_one(Hq, d):
     check(ph.Batch([900, 10, 64], [1, 1, 1], Hq, 1, d, "bf16", 16, seed=7), 100, 2, single=True)
