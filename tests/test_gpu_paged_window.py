@@ -231,6 +231,30 @@ def test_lengths_and_starts_out_of_range_stay_inside():
     assert torch.equal(out[0], vc[int(table[0, 0]), :, 0].repeat_interleave(2, 0))
 
 
+@pytest.mark.parametrize("d", [16, 64, 128])
+@pytest.mark.parametrize("window,sinks", [(20, 3), (1, 0), (2 ** 31 - 1, 0)])
+def test_lengths_out_of_range_of_single_tokens(d, window, sinks):
+    """More than the table holds, none, and what is no length: a token keeps its position and sees the keys that there are."""
+    lengths = [61, 2 ** 31 - 1, 0, -5, -2 ** 31, 48]
+    batch = ph.Batch([47] * 6, [1] * 6, 4, 2, d, "bf16", 16, seed=d)
+    q, kc, vc, table, _, _ = batch.gpu(True)
+    out, lse = binding.attn_paged_fwd(q, kc, vc, table, torch.tensor(lengths, dtype=torch.int32).cuda(), softmax_scale=batch.tau, window=window, sinks=sinks)
+    u = torch.finfo(batch.dtype).eps / 2
+    for b, n in enumerate(lengths):
+        k, v = batch.rows(batch.kc, b), batch.rows(batch.vc, b)
+        rows = [j for j in range(min(n, 48)) if j > n - 1 - window or j < sinks]
+        for h in range(4):
+            if not rows:
+                assert (out[b, h] == 0).all() and float(lse[h, b]) == -math.inf
+                continue
+            s = batch.tau * (k[rows, h // 2] @ batch.q[b, h].double())
+            w = torch.softmax(s, 0)
+            want, spread = w @ v[rows, h // 2], w @ v[rows, h // 2].abs()
+            # (the rounding of O, that of the probabilities in numerator and denominator, and logits in 32 bits)
+            assert ((out[b, h].cpu().double() - want).abs() <= u * want.abs() + (u + 2.0 ** -16) * (spread + want.abs()) + 2.0 ** -24).all()
+            assert abs(float(lse[h, b]) - float(torch.logsumexp(s, 0))) <= 1e-4
+
+
 def test_caches_beyond_32_bit_offsets():
     """More than 4 GiB of K: pages at both ends of the cache."""
     pages, Hk, page, d = 9000, 8, 256, 128
