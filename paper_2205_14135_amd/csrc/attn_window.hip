@@ -60,8 +60,9 @@ __device__ __forceinline__ void hide_far(const WindowArgs& a, f32x16 (&s)[2], in
 
 // RW wavefronts of 32 rows share the tiles of a workgroup, and KG groups of them work on the same rows, group k on every KG-th tile, in buffers of its own; their (m, l, O) are merged
 // through LDS at the end, as in attn_fwd.hip.
-template <typename T, int D, bool DROPOUT, int RW, int KG>
-__global__ __launch_bounds__(64 * RW * KG, KG == 1 && D <= 64 ? 3 : 2) void window_fwd_kernel(const WindowArgs w) {
+// PER_UNIT: workgroups, of four wavefronts, that a compute unit is to hold.
+template <typename T, int D, bool DROPOUT, int RW, int KG, int PER_UNIT>
+__global__ __launch_bounds__(64 * RW * KG, PER_UNIT) void window_fwd_kernel(const WindowArgs w) {
   typedef typename Vec<T>::x8 T8;
   constexpr int KK = D / 16, DB = D / 32, BR = 32 * RW, PF = 4;
   typedef T Tile[TILE * D];
@@ -467,12 +468,22 @@ bool window_divided(const WindowArgs& a, int64_t compute_units_blocks) {
   const int64_t blocks64 = (int64_t)a.k.B * a.k.H * ((a.k.N + 63) / 64);
   return blocks64 <= compute_units_blocks * kComputeUnits;
 }
+// (d = 64 in 128 registers, four workgroups to a compute unit instead of three, where there are more blocks than three to each; with dropout that spills.  us, heads x N, window, blocks, three | four:
+// 97 x 1024, 256, 776 25.8 | 22.7, 128 x 1024, 1024 28.5 | 26.4, 32 x 4096, 512, 1024 40.0 | 35.5, 128 x 2048, 1024, 2048 87.3 | 86.8, 300 x 1024, 128, 2400 42.8 | 40.8; 96 x 512, 100, 384 12.6 | 13.4, 64 x
+// 1024, 256, 512 16.4 | 16.9.)
 template <typename T, int D, int RW, int KG> int launch_fwd(WindowArgs a, bool dropout, hipStream_t s) {
+  constexpr int PER = KG == 1 && D <= 64 ? 3 : 2;
   a.k.n_items = a.k.B * a.k.H * ((a.k.N + 32 * RW - 1) / (32 * RW));
   a.k.chunk = (a.k.n_items + kXcds - 1) / kXcds;
   const dim3 grid(kXcds * a.k.chunk), block(64 * RW * KG);
-  if (dropout) hipLaunchKernelGGL((window_fwd_kernel<T, D, true, RW, KG>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((window_fwd_kernel<T, D, false, RW, KG>), grid, block, 0, s, a);
+  if constexpr (D == 64 && KG == 1) {
+    if (!dropout && a.k.n_items > PER * kComputeUnits) {
+      hipLaunchKernelGGL((window_fwd_kernel<T, D, false, RW, KG, PER + 1>), grid, block, 0, s, a);
+      return (int)hipGetLastError();
+    }
+  }
+  if (dropout) hipLaunchKernelGGL((window_fwd_kernel<T, D, true, RW, KG, PER>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((window_fwd_kernel<T, D, false, RW, KG, PER>), grid, block, 0, s, a);
   return (int)hipGetLastError();
 }
 template <typename T, int D, int RW, int KG> int launch_dq(WindowArgs a, bool dropout, hipStream_t s) {
