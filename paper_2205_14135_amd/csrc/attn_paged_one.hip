@@ -5,6 +5,8 @@
 // ends an item and waits for the page numbers and the first tile of the next, the others stream on.
 //   A tile is 32 keys of K and V.  S^T = K Q^T with 32x32x16 MFMA: a lane holds the logits of one row (G of the 32 are real), online softmax,
 // O^T += V^T P^T; the matrix and vector work is a fifth of what the memory takes.
+//   With a window (WINDOW) the tiles of an item are those that its rows see, the sinks' and the window's: 64 sequences of 500 to 30000 tokens, 32 / 8 heads of 128, window 2048 and four sinks, 443 MB
+// in 90 us (4.9 TB/s) and the join 5.
 //   A page holds 16 rows or more, so a tile has two page numbers at most, which scalar loads bring a tile ahead.
 #include "attn_paged_tiles.h"
 

@@ -1,6 +1,6 @@
 // dK and dV of attention with a sliding window and first tokens that stay visible, gfx950.
 //
-// Arithmetic and register layout are those of attn_bwd_dkv_fr128.hip (lane = key; one wavefront does all four tile products of its 32 keys). 
+// Arithmetic and register layout are those of attn_bwd_dkv_fr128.hip (lane = key; one wavefront does all four tile products of its 32 keys).
 // A block of 128 keys is swept by the (window + 128) / QT tiles of queries from the diagonal on, whatever the length.  What is left are the pairs of a sink and a query a window or more
 // behind it: few keys and many queries.  Either the blocks that hold sinks are swept by all queries (WindowArgs::swept_through), or workgroups in front of the others take 32 keys and a
 // stretch of the queries each, their four wavefronts every fourth tile of it, in buffers of their own (window_plan says which).
@@ -8,6 +8,8 @@
 // atomics, the same bits every time.
 // (The stretches in a launch of their own: us of the backward pass with four sinks 16 x 1024, window 256, d = 64 35.4 -> 25.6, 16 x 4096, 1024, d = 128 147 -> 131, 16 x 2048, 512 75 -> 58;
 // 16 x 16384, 1024, whose other blocks fill the chip four times exactly, the same.)
+// One MI355X, bf16: 16 heads x 16384, d = 128, window 1024, four sinks 290 us and the join 7.5 (920 TFLOP/s of the visible pairs' four products, matrix units busy in 50 per cent of the cycles);
+// 128 heads x 1024, d = 64, window 256, swept through, 40 us.
 // Vector registers: d = 128 keeps the V rows in LDS (as there) and 32 queries to a tile, d <= 64 both operands in registers and 64 queries.
 #include "attn_window.h"
 
@@ -31,7 +33,7 @@ template <typename T, int D, bool SINKS> struct DkvShape {
   static constexpr int kBytes = KG * kGroupBytes + (D == 128 ? BR * D * (int)sizeof(T) : 0);
 };
 
-// SINKS: a block of 32 keys and a stretch of queries, else a block of 128 keys.  place: of the workgroup among those of its kind.
+// SINKS: a block of 32 keys and a stretch of queries, else a block of 128 keys.  number: of the workgroup among those of its kind.
 template <typename T, int D, bool DROPOUT, bool SINKS>
 __device__ __forceinline__ void window_dkv_block(const WindowArgs& w, unsigned char* const all, uint32_t* const keep_table, const int number) {
   typedef typename Vec<T>::x8 T8;
