@@ -61,6 +61,7 @@ __device__ __forceinline__ void hide_far(const WindowArgs& a, f32x16 (&s)[2], in
   }
 }
 
+// Probabilities are rounded to 16 bits for their product with V and O is divided by the sum of the rounded ones, as in the dense forward; maxima, sums and O are in 32 bits until the one rounding at the end.
 // RW wavefronts of 32 rows share the tiles of a workgroup, and KG groups of them work on the same rows, group k on every KG-th tile, in buffers of its own; their (m, l, O) are merged
 // through LDS at the end, as in attn_fwd.hip.
 // PER_UNIT: workgroups, of four wavefronts, that a compute unit is to hold.
@@ -260,6 +261,8 @@ __global__ __launch_bounds__(64 * RW * KG, PER_UNIT) void window_fwd_kernel(cons
 }
 
 // dQ, and -D and the row statistic in base 2 for the dK/dV kernels, as in attn_bwd.hip.
+// S, dP, P and the sums are in 32 bits; dS is rounded to 16, half a step each, for its product with K, because the matrix unit takes 16-bit operands: dQ, itself rounded once, is off by 0.0025 of its norm in bf16 and 0.0003 in fp16,
+// where 32-bit arithmetic rounded once is off by 0.0017 and 0.0002.  (What the rounding drops as a second operand: a third more matrix products here for that factor of 1.5; the dense kernels round as this one does.)
 template <typename T, int D, bool DROPOUT, int RW, int KG>
 __global__ __launch_bounds__(64 * RW * KG, 2) void window_dq_kernel(const WindowArgs w) {
   typedef typename Vec<T>::x8 T8;
