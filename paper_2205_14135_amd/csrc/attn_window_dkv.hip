@@ -10,7 +10,7 @@
 // 16 x 16384, 1024, whose other blocks fill the chip four times exactly, the same.)
 // One MI355X, bf16: 16 heads x 16384, d = 128, window 1024, four sinks 290 us and the join 7.5 (920 TFLOP/s of the visible pairs' four products, matrix units busy in 50 per cent of the cycles);
 // 128 heads x 1024, d = 64, window 256, swept through, 40 us.
-// P and dS are rounded to 16 bits, half a step each, for their products with dO and Q, as in the dense kernels: dK and dV are off by 0.0024 of their norms in bf16, 0.0017 with 32-bit arithmetic rounded once.
+// P and dS are rounded to 16 bits, half a step each, for their products with dO and Q, as in the dense kernels: dK and dV are no further off than dQ (attn_window.hip).
 // Vector registers: d = 128 keeps the V rows in LDS (as there) and 32 queries to a tile, d <= 64 both operands in registers and 64 queries.
 #include "attn_window.h"
 
