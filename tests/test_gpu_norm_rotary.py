@@ -251,6 +251,26 @@ def test_a_training_step_in_a_captured_graph():
         assert all(torch.equal(a, b) for a, b in zip(got, want)), n
 
 
+@pytest.mark.parametrize("interleaved,r", [(False, 64), (False, 20), (True, 64)])
+def test_rows_and_heads_beyond_32_bit_offsets(interleaved, r):
+    """Tensors that span more than 4 GiB, by their rows and by their heads: the bits of packed ones."""
+    N, H, d = 300, 2, 64
+    gen = torch.Generator(device="cuda").manual_seed(r)
+    packed = [torch.randn(1, H, N, d, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(4)]
+    norm = HeadNorm(*(1.0 + 0.25 * torch.randn(d, generator=gen, device="cuda") for _ in range(2)))
+    rotary = Rotary.make(r, interleaved=interleaved)
+
+    def run(ts):
+        return [*binding.attn_norm_rotary(ts[0], ts[1], norm, rotary), *binding.attn_norm_rotary_bwd(*ts, norm, rotary)]
+
+    want = run(packed)
+    for strides in ((H * 256, 256, 1 << 23, 1), ((1 << 33), (1 << 31) + 1024, d, 1)):
+        far = [torch.empty_strided(x.shape, strides, dtype=x.dtype, device="cuda").copy_(x) for x in packed]
+        for got, exact in zip(run(far), want):
+            assert torch.equal(got, exact)
+        del far
+
+
 def test_on_another_stream():
     q, k, wq, wk, gq, gk, rotary = _leaves(N=3000)
     norm = HeadNorm(wq, wk)

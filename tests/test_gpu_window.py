@@ -90,6 +90,33 @@ def test_many_heads():
     _check(3, 11, 700, 64, "bf16", 200, 4, lengths=[700, 90, 400], heads=[(0, 0), (1, 3), (2, 10)])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("N,window,sinks,kw", [(100, 20, 2, {}), (130, 40, 0, dict(layout="token")), (100, 33, 3, dict(p=0.2)), (129, 64, 1, dict(lengths=[129, 70]))])
+def test_more_blocks_than_three_to_a_compute_unit(dtype, N, window, sinks, kw):
+    _check(2, 400, N, 64, dtype, window, sinks, heads=[(0, 0), (0, 399), (1, 7), (1, 368), (1, 399)], **kw)
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_rows_and_heads_beyond_32_bit_offsets(d):
+    """Tensors that span more than 4 GiB, by their rows and by their heads: the bits of packed ones."""
+    N, H = 300, 2
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    packed = [torch.randn(1, H, N, d, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(4)]
+    kw = dict(window=70, sinks=3, softmax_scale=d ** -0.5)
+
+    def run(ts):
+        O, L = binding.attn_window_fwd(*ts[:3], **kw)
+        return [O, L, *binding.attn_window_bwd(*ts[:3], O, ts[3], L, **kw)]
+
+    want = run(packed)
+    for strides in ((H * 256, 256, 1 << 23, 1), ((1 << 33), (1 << 31) + 1024, d, 1)):
+        far = [torch.empty_strided(x.shape, strides, dtype=x.dtype, device="cuda").copy_(x) for x in packed]
+        assert far[0].storage_offset() + sum((n - 1) * s for n, s in zip(far[0].shape, strides)) > 1 << 31
+        for got, exact in zip(run(far), want):
+            assert torch.equal(got, exact)
+        del far
+
+
 @pytest.mark.parametrize("d", [16, 32, 64, 128])
 @pytest.mark.parametrize("N,window,sinks,kw", [(300, 200, 4, {}), (300, 150, 140, {}), (333, 200, 40, dict(p=0.2)), (300, 200, 5, dict(lengths=[300, 17, 256, 129, 0, 299, 300])), (260, 130, 129, {})])
 def test_sinks_that_are_swept_through(d, N, window, sinks, kw):
