@@ -2,7 +2,8 @@
 //
 // Key j is visible to query i iff j <= i and (i - j < window or j < sinks).  The arithmetic is that of the causal kernels (attn_fwd.hip, attn_bwd.hip); a block of 128 rows sweeps the
 // tiles of 64 keys that hold sinks and those from the first one that its first row's window reaches to the diagonal: (window + 128) / 64 + 1 of them and the sinks', whatever the length.  Blocks cost
-// the same but for the first of a head, so that they are dealt out in order, neighbours to the same XCD, whose L2 has loaded most of their keys already.
+// the same but for the first of a head, which come last (16 x 16384, window 8192, d = 128: forward 847 -> 790 us, backward pass 2440 -> 2368; narrower windows the same); neighbours go to the same XCD, whose L2 has loaded
+// most of their keys already.
 // Masks are looked at in the tiles that the edges cross only, the diagonal, the window's far edge and the last sink; wavefronts whose 32 rows see nothing of a tile skip it.
 //   One MI355X, bf16, operations of the visible pairs: 16 heads x 16384, d = 128, window 1024 and four sinks forward 175 us (765 TFLOP/s; 19 tiles are swept for 16 of pairs: 930 of what is executed), dQ 235 (855); the
 // matrix and vector units bound it, matrix units busy in 41 and 47 per cent of the cycles.  128 heads x 1024, d = 64, window 256: 26 and 40 us: a block has 7 tiles, and what it waits for at its start and its end, and 16
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(64 * RW * KG, PER_UNIT) void window_fwd_kernel(cons
   const int item = xcd_item(a.n_items, a.chunk);
   if (item < 0) return;
   const int n_qt = (a.N + BR - 1) / BR;
-  const int bh = dealt_head(a, item / n_qt), qt = item % n_qt;
+  const int bh = dealt_head(a, item / n_qt), qt = n_qt - 1 - item % n_qt;
   const int b = bh / a.H, h = bh % a.H;
   const int64_t head_off = (int64_t)b * a.sb + (int64_t)h * a.sh;
   const T* __restrict__ Qg = (const T*)a.Q + head_off;
@@ -276,7 +277,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void window_dq_kernel(const Window
   const int item = xcd_item(a.n_items, a.chunk);
   if (item < 0) return;
   const int n_qt = a.T * (4 / RW);   // blocks of BR rows, to the end of the last 128-row block: the scratch vectors are written whole
-  const int bh = dealt_head(a, item / n_qt), qt = item % n_qt;
+  const int bh = dealt_head(a, item / n_qt), qt = n_qt - 1 - item % n_qt;
   const int b = bh / a.H, h = bh % a.H;
   const int64_t head_off = (int64_t)b * a.sb + (int64_t)h * a.sh;
   const T* __restrict__ Kg = (const T*)a.K + head_off;
