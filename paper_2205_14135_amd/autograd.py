@@ -58,7 +58,7 @@ class _WindowAttention(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, d_out):
         q, k, v, out, lse = ctx.saved_tensors
-        if d_out.shape != q.shape or d_out.stride() != q.stride():
+        if d_out.shape != q.shape or d_out.stride() != q.stride() or d_out.data_ptr() % 16 != 0:
             d_out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=q.device).copy_(d_out)
         return (*binding.attn_window_bwd(q, k, v, out, d_out, lse, **ctx.kw), *(None,) * 7)
 

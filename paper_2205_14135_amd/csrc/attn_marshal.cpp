@@ -260,7 +260,8 @@ struct WindowAttentionBackward : torch::autograd::Node {
     // (hooks of the program may have handed back something else than what was saved)
     const at::Tensor& x = t[0];
     at::Tensor d_out = grads[0];
-    if (x.sizes() == d_out.sizes() && x.strides() != d_out.strides()) d_out = like(x, x.scalar_type()).copy_(d_out);   // the library addresses dO with the strides of q
+    // The library addresses dO with the strides of q, and reads 16 bytes at a time: what a concatenation hands back, a view somewhere in a longer gradient, may start anywhere.
+    if (x.sizes() == d_out.sizes() && (x.strides() != d_out.strides() || ((uintptr_t)d_out.data_ptr() & 15u) != 0)) d_out = like(x, x.scalar_type()).copy_(d_out);
     check_saved(x, t[1], t[2], d_out, a);
     if (x.size(0) != p.B || x.size(1) != p.H || x.size(2) != p.N || x.size(3) != p.d || (x.scalar_type() == at::kHalf ? ATTN_FP16 : ATTN_BF16) != p.dtype || !alike(x, t[3]) ||
         t[3].scalar_type() != x.scalar_type() || t[1].scalar_type() != x.scalar_type() || t[2].scalar_type() != x.scalar_type() || d_out.scalar_type() != x.scalar_type() ||
