@@ -63,6 +63,12 @@ class _WindowAttention(torch.autograd.Function):
         return (*binding.attn_window_bwd(q, k, v, out, d_out, lse, **ctx.kw), *(None,) * 7)
 
 
+def _packed(x):
+    # what the library can read: rows in one piece that start on 16 bytes (contiguous() leaves a view at an odd offset as it is)
+    x = x.contiguous()
+    return x if x.data_ptr() % 16 == 0 else x.clone()
+
+
 class _RotaryEmbedding(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, frequencies, interleaved, magnitude, positions, inverse):
@@ -77,7 +83,7 @@ class _RotaryEmbedding(torch.autograd.Function):
         interleaved, magnitude, inverse = ctx.kw
         if frequencies.shape != ctx.pairs:
             raise ValueError("the saved frequencies or positions are not those of the forward call")
-        return (*_RotaryEmbedding.apply(d_q.contiguous(), d_k.contiguous(), frequencies, interleaved, magnitude, positions, not inverse), None, None, None, None, None)
+        return (*_RotaryEmbedding.apply(_packed(d_q), _packed(d_k), frequencies, interleaved, magnitude, positions, not inverse), None, None, None, None, None)
 
 
 class _NormRotaryEmbedding(torch.autograd.Function):
@@ -94,7 +100,7 @@ class _NormRotaryEmbedding(torch.autograd.Function):
         q, k, q_weight, k_weight, frequencies, positions = ctx.saved_tensors
         eps, interleaved, magnitude = ctx.kw
         rotary = None if frequencies is None else Rotary(frequencies, interleaved=interleaved, magnitude=magnitude)
-        grads = binding.attn_norm_rotary_bwd(q, k, d_q.contiguous(), d_k.contiguous(), HeadNorm(q_weight, k_weight, eps=eps), rotary, positions=positions)
+        grads = binding.attn_norm_rotary_bwd(q, k, _packed(d_q), _packed(d_k), HeadNorm(q_weight, k_weight, eps=eps), rotary, positions=positions)
         return (*grads, None, None, None, None, None)
 
 

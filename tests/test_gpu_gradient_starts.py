@@ -3,7 +3,8 @@ import pytest
 import torch
 
 from paper_2205_14135_amd import autograd
-from paper_2205_14135_amd.autograd import flash_attention
+from paper_2205_14135_amd.autograd import flash_attention, norm_rotary_embedding, rotary_embedding
+from paper_2205_14135_amd.rotary import HeadNorm, Rotary
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +52,28 @@ def test_window_behind_a_concatenation(node):
     out = _window(leaves, node, 40)
     got = torch.autograd.grad(torch.cat([first, out.flatten()]), leaves, torch.cat([first, do.flatten()]))
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def _turned(q, k, weights, node, normed):
+    if normed:
+        norm, rotary = HeadNorm(*weights), Rotary.make(64)
+        if node == "native":
+            return norm_rotary_embedding(q, k, norm, rotary)
+        return autograd._NormRotaryEmbedding.apply(q, k, *weights, norm.eps, rotary.frequencies, False, 1.0, None)
+    rotary = Rotary.make(64)
+    if node == "native":
+        return rotary_embedding(q, k, rotary)
+    return autograd._RotaryEmbedding.apply(q, k, rotary.frequencies, False, 1.0, None, False)
+
+
+@pytest.mark.parametrize("normed", [False, True])
+@pytest.mark.parametrize("node", ["native", "python"])
+def test_rotation(node, normed):
+    q, k, gq, gk = _tensors(3, 1, 3, 1)
+    weights = [torch.linspace(0.5, 1.5, 64, device="cuda", requires_grad=normed) for _ in range(2)]
+    leaves = [q.requires_grad_(True), k.requires_grad_(True)] + (weights if normed else [])
+    ys = _turned(q, k, weights, node, normed)
+    want = torch.autograd.grad(ys, leaves, (gq, gk), retain_graph=True)
+    for elements in (1, 4, 7, 8):
+        got = torch.autograd.grad(ys, leaves, [_moved(g, elements) for g in (gq, gk)], retain_graph=True)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), elements
