@@ -49,18 +49,18 @@ class _FlashAttention(torch.autograd.Function):
 class _WindowAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, softmax_scale, dropout_p, seed, offset, key_lengths, window, sinks):
-        ctx.kw = dict(softmax_scale=softmax_scale, dropout_p=dropout_p, seed=seed, offset=offset, key_lengths=key_lengths, window=window, sinks=sinks)
-        out, lse = binding.attn_window_fwd(q, k, v, **ctx.kw)
-        ctx.save_for_backward(q, k, v, out, lse)
+        ctx.kw = dict(softmax_scale=softmax_scale, dropout_p=dropout_p, seed=seed, offset=offset, window=window, sinks=sinks)
+        out, lse = binding.attn_window_fwd(q, k, v, key_lengths=key_lengths, **ctx.kw)
+        ctx.save_for_backward(q, k, v, out, lse, key_lengths)
         return out
 
     @staticmethod
     @once_differentiable
     def backward(ctx, d_out):
-        q, k, v, out, lse = ctx.saved_tensors
+        q, k, v, out, lse, key_lengths = ctx.saved_tensors
         if d_out.shape != q.shape or d_out.stride() != q.stride() or d_out.data_ptr() % 16 != 0:
             d_out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=q.device).copy_(d_out)
-        return (*binding.attn_window_bwd(q, k, v, out, d_out, lse, **ctx.kw), *(None,) * 7)
+        return (*binding.attn_window_bwd(q, k, v, out, d_out, lse, key_lengths=key_lengths, **ctx.kw), *(None,) * 7)
 
 
 def _packed(x):
