@@ -74,18 +74,20 @@ template <typename T, Pairing P> struct NormUnit {
       v[8 + e] = (float)b[e];
     }
   }
-  // v turned; other: the partners (kHalvesAny)
+  // v turned; other: the partners (kHalvesAny).  What does not turn stays as it is, as in attn_turn.h: cosine 1 and sine 0 would make NaN of it where an infinity stands in the other
+  // column, and lose the sign of zeros.  (us, products | this | a branch around what does not turn: 16384 tokens of 16 + 4 heads of 128, halves of them turning, neighbours 31.0 | 30.3 | 30.4, halves 29.6 | 29.8 | 29.9, backward
+  // 45.5 | 45.4 | 45.6 and 44.6 | 44.9 | 44.9; 197 tokens of 12 + 12 heads of 64 5.1 | 5.3 | 5.9.)
   __device__ __forceinline__ void apply(float (&v)[16], const float (&other)[P == kHalvesAny ? 16 : 1]) const {
     if constexpr (P == kHalvesAny) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = v[e] * turn.cs[e] + other[e] * turn.sn[e];
+      for (int e = 0; e < 16; ++e) v[e] = e < 2 * turn.turning ? v[e] * turn.cs[e] + other[e] * turn.sn[e] : v[e];
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float &a = P == kHalves ? v[e] : v[2 * e], &b = P == kHalves ? v[8 + e] : v[2 * e + 1];
         const float fa = a, fb = b;
-        a = fa * turn.cs[e] - fb * turn.sn[e];
-        b = fb * turn.cs[e] + fa * turn.sn[e];
+        a = e < turn.turning ? fa * turn.cs[e] - fb * turn.sn[e] : fa;
+        b = e < turn.turning ? fb * turn.cs[e] + fa * turn.sn[e] : fb;
       }
     }
   }
