@@ -371,7 +371,7 @@ size_t attn_norm_rotary_bwd_workspace_bytes(int32_t d);
 /*
  * With g = dy turned back and h = g o w:  dx = r (h - x r^2 mean(h o x)),  dw = the sum over all rows of g o x r,  r = 1 / sqrt(mean(x^2) + eps).
  * p and norm as in the forward call.  workspace: 256-byte aligned, needed where a dw is asked for; contents on entry are ignored.  The same inputs give the same bits in every
- * call.
+ * call.  A finite row whose squares add up beyond 32 bits has no gradient, as it has come out as zeros: its dx is 0, and it adds nothing to dw.
  */
 int attn_norm_rotary_bwd(const attn_rotary_params* p, const attn_norm_spec* norm, const attn_norm_grad* tensors, int32_t n_tensors, void* workspace,
                          size_t workspace_bytes);

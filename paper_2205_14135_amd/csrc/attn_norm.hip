@@ -266,6 +266,16 @@ __global__ __launch_bounds__(NT, P == kHalvesAny ? 2 : 3) void norm_rotary_bwd_k
         hx += gv[e] * unit.w[e] * v[e];
       }
       const float r = 1.f / sqrtf(row_sum(ss, units_log2) * inv_d + c.norm.eps);
+      if (__builtin_expect(r == 0.f, 0)) {
+        // Squares beyond 32 bits: the forward pass made zeros of a finite row, and it has no gradient.  (Its products with h may be infinities, 0 times which would be in dx and in all rows' dw.)  What
+        // is infinite in x itself becomes NaN here, and all of dx with it.
+        hx = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          v[e] *= r;
+          hx += gv[e] * unit.w[e] * v[e];
+        }
+      }
       const float back = row_sum(hx, units_log2) * inv_d * r * r;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {

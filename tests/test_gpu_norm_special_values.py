@@ -132,3 +132,36 @@ def test_append(d, r, interleaved):
     _same(kc[torch.tensor([2, 0, 1])].transpose(1, 2).reshape(48, H, d)[:N].cpu(), want, "K")
     exact, _ = nh.forward(x, w, EPS, torch.arange(N), f, interleaved)
     _same(want[BAD, 1], exact[BAD, 1], "the rows with an infinity")
+
+
+@pytest.mark.parametrize("d,r,interleaved", FORMS)
+@pytest.mark.parametrize("exponent,columns", [(66, None), (126, None), (64, 1), (127, 1)])
+def test_squares_beyond_32_bits(d, r, interleaved, exponent, columns):
+    """Finite rows whose squares add up beyond float32 come out as zeros and have no gradient: not in their own elements, and not in that of the weights."""
+    x, dy, w, f, rotary = _case(d, r, interleaved, "bf16")
+    dy = dy * 16.0
+    large, none = x.clone(), x.clone()
+    large[BAD, 1, :columns] = torch.where(x[BAD, 1, :columns] < 0, -(2.0 ** exponent), 2.0 ** exponent).to(x.dtype)
+    none[BAD, 1] = 0.0
+    got, want = _forward(large, w, rotary), _forward(none, w, rotary)
+    assert (got[BAD, 1] == 0).all() and torch.equal(got, want)
+    (dx, dw), (want, want_w) = _backward(large, dy, w, rotary), _backward(none, dy, w, rotary)
+    assert (dx[BAD, 1] == 0).all() and torch.equal(dw, want_w)
+    want[BAD, 1] = 0.0
+    assert torch.equal(dx, want)
+
+
+@pytest.mark.parametrize("d,r,interleaved", FORMS)
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_rows_that_are_no_numbers_have_no_gradients_either(d, r, interleaved, value):
+    """(by the formula: 0 times an infinity is in every element of such a row, and in every column of the weights' gradient that it has a part in)"""
+    x, dy, w, f, rotary = _case(d, r, interleaved, "bf16")
+    x[BAD[1], 1, d // 2] = value
+    want, bound, want_w, bound_w = nh.gradients(x, w, dy, EPS, torch.arange(N), f, interleaved)
+    got, got_w = _backward(x, dy, w, rotary)
+    rest = [n for n in range(N) if n != BAD[1]]
+    ph.assert_within(got[rest], want[rest], bound[rest], "other rows")
+    assert torch.isnan(want[BAD[1], 1]).all() and torch.isnan(got[BAD[1], 1]).all()
+    numbers = ~torch.isnan(want_w)
+    assert torch.equal(~torch.isnan(got_w), numbers)
+    ph.assert_within(got_w[numbers], want_w[numbers], bound_w[numbers], "weights")
