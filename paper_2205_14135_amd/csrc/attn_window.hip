@@ -91,6 +91,9 @@ __global__ __launch_bounds__(64 * RW * KG, PER_UNIT) void window_fwd_kernel(cons
   const int q0 = qt * BR + wave * 32;
   const bool row_ok = q0 + r < a.N;   // (lanes beyond a ragged end work on a copy of the last row and store nothing)
   const int qi = min(q0 + r, a.N - 1);
+  // What stands at padded positions is not read: the last row that is none stands for it, so that nothing but finite numbers meets the weights 0.
+  const int len = a.klen ? min(max(a.klen[b], 0), a.N) : a.N;
+  const int q_row = min(qi, max(len - 1, 0));
 
   T8 qf[KK];   // Q^T fragments (B operand): query qi, d = 16 kk + 8 g .. +7
 #pragma unroll
@@ -99,7 +102,7 @@ __global__ __launch_bounds__(64 * RW * KG, PER_UNIT) void window_fwd_kernel(cons
 #pragma unroll
       for (int e = 0; e < 8; ++e) qf[kk][e] = (T)0.f;
     } else {
-      qf[kk] = *(const T8*)(Qg + (int64_t)qi * a.sn + 16 * kk + 8 * g);
+      qf[kk] = *(const T8*)(Qg + (int64_t)q_row * a.sn + 16 * kk + 8 * g);
     }
   }
   f32x16 o[DB];
@@ -112,7 +115,6 @@ __global__ __launch_bounds__(64 * RW * KG, PER_UNIT) void window_fwd_kernel(cons
   int calm = kFirstTile;
   const T8 ones = row_sum_ones<T>();
 
-  const int len = a.klen ? min(max(a.klen[b], 0), a.N) : a.N;
   WindowTiles it;
   it.init<BR>(w, qt * BR, len);
   TrOffsets<D> tro;
@@ -127,8 +129,8 @@ __global__ __launch_bounds__(64 * RW * KG, PER_UNIT) void window_fwd_kernel(cons
   int jt, buf = 0;   // this group's tile, -1 if there is none; more: some group (then the first) has one
   bool more = it.next_of<KG>(group, jt);
   if (jt >= 0) {
-    dma.copy_rows(Kg, a.sn, jt * TILE, a.N, Ks[2 * group]);
-    dma.copy_rows(Vg, a.sn, jt * TILE, a.N, Vs[2 * group]);
+    dma.copy_rows(Kg, a.sn, jt * TILE, len, Ks[2 * group]);
+    dma.copy_rows(Vg, a.sn, jt * TILE, len, Vs[2 * group]);
   }
   wait_async_copies();
   __syncthreads();   // the first tile has landed, and so have the Q fragments
@@ -143,8 +145,8 @@ __global__ __launch_bounds__(64 * RW * KG, PER_UNIT) void window_fwd_kernel(cons
     int jn;
     const bool more_next = it.next_of<KG>(group, jn);
     if (jn >= 0) {   // the next tile streams into the other buffer while this one is used
-      dma.copy_rows(Kg, a.sn, jn * TILE, a.N, Ks[2 * group + (buf ^ 1)]);
-      dma.copy_rows(Vg, a.sn, jn * TILE, a.N, Vs[2 * group + (buf ^ 1)]);
+      dma.copy_rows(Kg, a.sn, jn * TILE, len, Ks[2 * group + (buf ^ 1)]);
+      dma.copy_rows(Vg, a.sn, jn * TILE, len, Vs[2 * group + (buf ^ 1)]);
     }
     const T* Vt = Vs[2 * group + buf];
     const int k0 = jt * TILE;
@@ -287,12 +289,14 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void window_dq_kernel(const Window
   const int q0 = qt * BR + wave * 32;
   const bool row_ok = q0 + r < a.N;
   const int qi = min(q0 + r, a.N - 1);
+  const int len = a.klen ? min(max(a.klen[b], 0), a.N) : a.N;
+  const int q_row = min(qi, max(len - 1, 0));   // (as in the forward pass)
 
   T8 qf[KK], gf[KK];   // Q^T and dO^T fragments of this lane's query
   float d_part = 0.f;
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) {
-    const int64_t off = head_off + (int64_t)qi * a.sn + 16 * kk + 8 * g;
+    const int64_t off = head_off + (int64_t)q_row * a.sn + 16 * kk + 8 * g;
     if (D == 32 && 16 * kk + 8 * g >= a.dvalid) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) { qf[kk][e] = (T)0.f; gf[kk][e] = (T)0.f; }
@@ -324,7 +328,6 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void window_dq_kernel(const Window
 #pragma unroll
     for (int i = 0; i < 16; ++i) dq[db][i] = 0.f;
 
-  const int len = a.klen ? min(max(a.klen[b], 0), a.N) : a.N;
   WindowTiles it;
   it.init<BR>(w, qt * BR, len);
   TrOffsets<D> tro;
@@ -339,8 +342,8 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void window_dq_kernel(const Window
   int jt, buf = 0;
   bool more = it.next_of<KG>(group, jt);
   if (jt >= 0) {
-    dma.copy_rows(Kg, a.sn, jt * TILE, a.N, Ks);
-    dma.copy_rows(Vg, a.sn, jt * TILE, a.N, Vs);
+    dma.copy_rows(Kg, a.sn, jt * TILE, len, Ks);
+    dma.copy_rows(Vg, a.sn, jt * TILE, len, Vs);
   }
   wait_async_copies();
   __syncthreads();
@@ -348,8 +351,8 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void window_dq_kernel(const Window
     int jn;
     const bool more_next = it.next_of<KG>(group, jn);
     if (jn >= 0) {
-      dma.copy_rows(Kg, a.sn, jn * TILE, a.N, Ks + (buf ^ 1) * TILE * D);
-      dma.copy_rows(Vg, a.sn, jn * TILE, a.N, Vs + (buf ^ 1) * TILE * D);
+      dma.copy_rows(Kg, a.sn, jn * TILE, len, Ks + (buf ^ 1) * TILE * D);
+      dma.copy_rows(Vg, a.sn, jn * TILE, len, Vs + (buf ^ 1) * TILE * D);
     }
     const T* Kt = Ks + buf * TILE * D;
     const T* Vt = Vs + buf * TILE * D;

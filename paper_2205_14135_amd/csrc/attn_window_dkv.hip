@@ -68,9 +68,11 @@ __device__ __forceinline__ void window_dkv_block(const WindowArgs& w, unsigned c
   const int lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5;
   const int kb0 = kt * BR, kw0 = kb0 + wave * 32, kj = kw0 + r;
 
+  // (what stands at padded positions is not read, as in the forward pass: the last row that is none stands for it)
+  const int len = a.klen ? min(max(a.klen[b], 0), a.N) : a.N;
   T8 kf[KK], vf[V_IN_LDS ? 1 : KK];
   {
-    const int64_t row_off = head_off + (int64_t)min(kj, a.N - 1) * a.sn;
+    const int64_t row_off = head_off + (int64_t)min(kj, max(len - 1, 0)) * a.sn;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
       if (D == 32 && 16 * kk + 8 * g >= a.dvalid) {   // head dimension 16: the upper columns are zeros
@@ -89,7 +91,6 @@ __device__ __forceinline__ void window_dkv_block(const WindowArgs& w, unsigned c
 #pragma unroll
     for (int i = 0; i < 16; ++i) { dv[db][i] = 0.f; dk[db][i] = 0.f; }
 
-  const int len = a.klen ? min(max(a.klen[b], 0), a.N) : a.N;
   // Tiles of queries first .. limit - 1
   int first, limit = (len + QT - 1) / QT;
   if constexpr (SINKS) {
@@ -111,22 +112,22 @@ __device__ __forceinline__ void window_dkv_block(const WindowArgs& w, unsigned c
     __syncthreads();
   }
   auto fetch_tile = [&](int t, int buf) {
-    dma.copy_rows(Qg, a.sn, t * QT, a.N, Qs0 + buf * QT * D);
-    dma.copy_rows(Gg, a.sn, t * QT, a.N, Gs0 + buf * QT * D);
+    dma.copy_rows(Qg, a.sn, t * QT, len, Qs0 + buf * QT * D);
+    dma.copy_rows(Gg, a.sn, t * QT, len, Gs0 + buf * QT * D);
     const int row = min(t * QT + lane, a.Nr - 1);   // whole-wavefront copies: 64 floats, clamped to the head
     if (wave == (RW - 1) / 2) async_copy_b32(Lg + row, __builtin_amdgcn_readfirstlane(lds_addr(Ls0 + 64 * buf)));
     if (wave == RW / 2) async_copy_b32(Dg + row, __builtin_amdgcn_readfirstlane(lds_addr(Ds0 + 64 * buf)));
   };
   const float c = a.scale_log2;
-  if constexpr (V_IN_LDS) {   // (rows >= N repeat the last one; their keys are masked)
+  if constexpr (V_IN_LDS) {   // (rows >= len repeat the last one; their keys are masked)
     constexpr int VR = BR < 64 ? BR : 64;
     TileAsync<T, D, RW, VR> dma_v;
     dma_v.init(a.sn, wave);
     if (group == 0) {
-      if (kb0 < a.N) dma_v.copy_rows(Vg, a.sn, kb0, a.N, Vb);
+      if (kb0 < len) dma_v.copy_rows(Vg, a.sn, kb0, len, Vb);
       if constexpr (BR > 64) {
-        if (kb0 + 64 < a.N) dma_v.copy_rows(Vg, a.sn, kb0 + 64, a.N, Vb + 64 * D);
-        else if (kb0 < a.N) dma_v.copy_rows(Vg, a.sn, kb0, a.N, Vb + 64 * D);   // all of these keys are masked
+        if (kb0 + 64 < len) dma_v.copy_rows(Vg, a.sn, kb0 + 64, len, Vb + 64 * D);
+        else if (kb0 < len) dma_v.copy_rows(Vg, a.sn, kb0, len, Vb + 64 * D);   // all of these keys are masked
       }
     }
   }
