@@ -134,6 +134,19 @@ def test_few_rows_are_worked_on_apart(new):
     check(ph.Batch([(b * 1237) % 3000 for b in range(B)], new, 32, 16, 128, "fp16", 256, pad=3, seed=31), 2600, 1900)
 
 
+@pytest.mark.parametrize("new", [[1, 500, 1, 16, 17, 0, 1, 9], [40, 33, 300, 64], [1] * 7 + [900]])
+@pytest.mark.parametrize("dtype,page,window,sinks", [("fp16", 256, 2600, 1900), ("bf16", 64, 100, 4400), ("fp16", 16, 4096, 4)])
+def test_few_rows_apart_with_many_sinks(new, dtype, page, window, sinks):
+    """The same two passes over wide pages, and with sinks of many tiles."""
+    B = len(new)
+    batch = ph.Batch([(b * 1237) % 3000 for b in range(B)], new, 32, 16, 128, dtype, page, pad=3, seed=31)
+    wide = torch.full((B, 5120 // page), -1, dtype=torch.int32)
+    wide[:, :batch.table.shape[1]] = batch.table
+    batch.table = wide
+    assert sum(new) * 2 > 32 * B and 16 * (B - 1) * min(5120, window + sinks) >= 3000 * 64       # (larger blocks, and the rule's bound)
+    check(batch, window, sinks)
+
+
 @pytest.mark.parametrize("new", [[2, 3, 1], [1, 1, 1]])
 def test_few_tokens_with_starts(new):
     check(ph.Batch([600, 20, 2100], new, 8, 2, 128, "bf16", 16, pad=2, seed=6), 250, 3)
