@@ -74,22 +74,29 @@ template <typename T, Pairing P> struct NormUnit {
       v[8 + e] = (float)b[e];
     }
   }
-  // v turned; other: the partners (kHalvesAny).  What does not turn stays as it is, as in attn_turn.h: cosine 1 and sine 0 would make NaN of it where an infinity stands in the other
-  // column, and lose the sign of zeros.  (us, products | this | a branch around what does not turn: 16384 tokens of 16 + 4 heads of 128, halves of them turning, neighbours 31.0 | 30.3 | 30.4, halves 29.6 | 29.8 | 29.9, backward
-  // 45.5 | 45.4 | 45.6 and 44.6 | 44.9 | 44.9; 197 tokens of 12 + 12 heads of 64 5.1 | 5.3 | 5.9.)
-  __device__ __forceinline__ void apply(float (&v)[16], const float (&other)[P == kHalvesAny ? 16 : 1]) const {
+  // v with all of its pairs turned; other: the partners (kHalvesAny)
+  __device__ __forceinline__ void turn_all(float (&v)[16], const float (&other)[P == kHalvesAny ? 16 : 1]) const {
     if constexpr (P == kHalvesAny) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = e < 2 * turn.turning ? v[e] * turn.cs[e] + other[e] * turn.sn[e] : v[e];
+      for (int e = 0; e < 16; ++e) v[e] = v[e] * turn.cs[e] + other[e] * turn.sn[e];
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float &a = P == kHalves ? v[e] : v[2 * e], &b = P == kHalves ? v[8 + e] : v[2 * e + 1];
         const float fa = a, fb = b;
-        a = e < turn.turning ? fa * turn.cs[e] - fb * turn.sn[e] : fa;
-        b = e < turn.turning ? fb * turn.cs[e] + fa * turn.sn[e] : fb;
+        a = fa * turn.cs[e] - fb * turn.sn[e];
+        b = fb * turn.cs[e] + fa * turn.sn[e];
       }
     }
+  }
+  // The same, but what does not turn stays as it is, as in attn_turn.h: cosine 1 and sine 0 would make NaN of it where an infinity stands in the other column, and lose the sign of zeros.
+  __device__ __forceinline__ void apply(float (&v)[16], const float (&other)[P == kHalvesAny ? 16 : 1]) const {
+    float was[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) was[e] = v[e];
+    turn_all(v, other);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = (P == kHalves ? e & 7 : e / 2) < turn.turning ? v[e] : was[e];
   }
   static __device__ __forceinline__ void narrow(const float (&v)[16], T8& a, T8& b) {
 #pragma unroll
@@ -97,6 +104,23 @@ template <typename T, Pairing P> struct NormUnit {
       a[e] = (T)v[e];
       b[e] = (T)v[8 + e];
     }
+  }
+  // apply and narrow, the selection two rounded columns at a time.  us, all columns by products alone | a column at a time, in 32 bits | this: 197 tokens of 12 + 12 heads of 64 5.1 | 5.3 | 5.1, 64 tokens appended 5.1 | 5.3 | 5.2,
+  // 8 x 1024 of 16 + 16 heads of 64 14.0 | 14.1 | 14.2, 16384 of 16 + 4 of 128, halves of them turning, 28.9 | 29.1 | 29.1, neighbours 29.8 | 30.4 | 30.4.
+  __device__ __forceinline__ void apply_and_narrow(float (&v)[16], const float (&other)[P == kHalvesAny ? 16 : 1], T8& a, T8& b) const {
+    narrow(v, a, b);
+    turn_all(v, other);
+    T8 ta, tb;
+    narrow(v, ta, tb);
+    const u32x4 ua = __builtin_bit_cast(u32x4, a), ub = __builtin_bit_cast(u32x4, b);
+    u32x4 va = __builtin_bit_cast(u32x4, ta), vb = __builtin_bit_cast(u32x4, tb);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      va[i] = i < turn.turning ? va[i] : ua[i];
+      vb[i] = i + 4 < turn.turning ? vb[i] : ub[i];
+    }
+    a = __builtin_bit_cast(T8, va);
+    b = __builtin_bit_cast(T8, vb);
   }
   // Heads h0 .. h1 - 1 of one token, x and y at head 0; STREAM: past the caches, as in attn_turn.h.  y may be x: all threads of a row are in one wavefront, whose loads are
   // complete before its stores.
@@ -124,8 +148,7 @@ template <typename T, Pairing P> struct NormUnit {
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) v[e] = v[e] * r * w[e];
-        apply(v, other);
-        narrow(v, a[k], b[k]);
+        apply_and_narrow(v, other, a[k], b[k]);
       }
 #pragma unroll
       for (int k = 0; k < N; ++k) {
