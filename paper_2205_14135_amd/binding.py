@@ -338,7 +338,8 @@ def attn_window_fwd(Q, K, V, *, window, sinks=0, softmax_scale, dropout_p=0.0, s
 
 
 def attn_window_bwd_workspace_bytes(p: AttnParams, window: int, sinks: int = 0) -> int:
-    return int(load().attn_window_bwd_workspace_bytes(ctypes.byref(p), int(window), int(sinks)))
+    within = lambda n: max(-2 ** 31, min(int(n), 2 ** 31 - 1))  # noqa: E731   (as the calls take them; ctypes would keep the low 32 bits)
+    return int(load().attn_window_bwd_workspace_bytes(ctypes.byref(p), within(window), within(sinks)))
 
 
 def attn_window_bwd(Q, K, V, O, dO, LSE, *, window, sinks=0, softmax_scale, dropout_p=0.0, seed=0, offset=0, o_fp32=False, workspace=None, grads=None, stream=None,

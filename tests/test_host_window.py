@@ -126,3 +126,15 @@ def test_paged_marshalling(lib):
                       (dict(sinks=3), ValueError), (dict(window=1.5), TypeError), (dict(window=4), RuntimeError)):
         with pytest.raises(error):
             binding.attn_paged_fwd(q, c, c, t, n, softmax_scale=0.1, **kw)
+
+
+def test_workspace_of_windows_beyond_32_bits(lib):
+    """(as the calls take them: kept within 32 bits, not cut to their low ones)"""
+    p = _params()
+    nbytes = binding.attn_window_bwd_workspace_bytes
+    all_keys, few = nbytes(p, 512, 0), nbytes(p, 64, 4)
+    assert all_keys > 0 and few > 0
+    for window in (2 ** 31 - 1, 2 ** 31, 2 ** 32 + 1, 10 ** 12):
+        assert nbytes(p, window, 0) == all_keys
+        assert nbytes(p, 64, window) == all_keys
+        assert nbytes(p, -window, 0) == 0 and nbytes(p, 64, -window) == 0
