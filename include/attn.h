@@ -218,7 +218,10 @@ int attn_blocksparse_bwd(const attn_params* p, const uint8_t* block_mask, int32_
  */
 int attn_window_fwd(const attn_params* p, int32_t window, int32_t sinks, const void* Q, const void* K, const void* V, void* O, float* LSE);
 
-/* Bytes of scratch for attn_window_bwd: what attn_bwd needs, and pieces of dK and dV in float32 for the keys that are sinks (32 at a time).  0 if the params are invalid. */
+/*
+ * Bytes of scratch for attn_window_bwd: two floats a row (N rounded up to 128), and pieces of dK and dV in float32 for the keys that are sinks, 32 at a time: 256 d bytes each, at least two for
+ * every head and 32 sinks, or none.  Where nothing is hidden, attn_bwd_workspace_bytes.  0 if the params are invalid.
+ */
 size_t attn_window_bwd_workspace_bytes(const attn_params* p, int32_t window, int32_t sinks);
 
 /* Its backward pass: arguments as attn_bwd, O and LSE from attn_window_fwd.  Gradients are the same bits in every call. */

@@ -7,9 +7,11 @@
 // Memory bounds all of it: 4 bytes a column forward, 6 backward, each row read and written once.  A thread has 16 columns of one token and walks over heads, as in
 // attn_rotary.hip, so that its angles and its 16 weights serve all of them; the d / 16 threads of a row are neighbours in a wavefront and add their
 // shares of a row's sums by cross-lane moves.  All arithmetic between the load and the one rounding at the end is in 32 bits.
-// One MI355X: 16384 tokens of 16 + 4 heads of 128 in fp16, half of each row turning, forward 33 us (168 MB, 5.1 TB/s), backward 53 + 4 us (252 MB, 4.7 TB/s in the first launch); 12 prompts of up to 2048
-// tokens appended, 16 heads of 64, 16.6 us (91 MB, 5.5 TB/s); 64 single tokens of 32 + 8 heads of 128 5.5 us, a launch and the chain length, angles, row, store.  (Rows loaded ahead of the angles: 5.4 -> 6.4 us for 197
-// tokens of 12 + 12 heads of 64, 33 -> 35 us for the 16384.)
+// One MI355X: 16384 tokens of 16 + 4 heads of 128 in fp16, half of each row turning, forward 33 us (168 MB, 5.1 TB/s), backward 54 + 4 us (252 MB, 4.7 TB/s in the first launch); 12 prompts of up to 2048
+// tokens appended, 16 heads of 64, 16.9 us (91 MB, 5.4 TB/s); 64 single tokens of 32 + 8 heads of 128 5.4 us, a launch and the chain length, angles, row, store.  (Rows loaded ahead of the angles: 5.4 -> 6.4 us for 197
+// tokens of 12 + 12 heads of 64, 33 -> 35 us for the 16384.)  (Times of a trace; among others in a replayed graph the single tokens take 5.2.)
+// Halves with r no multiple of 16 read every partner by itself, two bytes at a time, and keep 246 to 256 registers: 16384 tokens of 16 + 4 heads of 64 in bf16, 20 columns turning, forward 53 us (84 MB, 1.6 TB/s), backward 65
+// (126 MB, 1.9 TB/s), where neighbours take 17 and 30.
 //   dw: a thread adds up its own rows, a workgroup its threads', and a second launch the workgroups' sums, each in a fixed order: the same inputs give the same bits.
 #include "attn_turn.h"
 

@@ -139,8 +139,8 @@ inline bool paged_window_apart(const attn_paged_params& p, const PagedShape& sha
   const int64_t reach = (int64_t)window + sinks, capacity = (int64_t)p.table_width * p.page_size;
   return shape.rows == 256 && (int64_t)p.Hk * (p.B - 1) * (reach < capacity ? reach : capacity) >= 3000 * 64;
 }
-// With a window and one new token a sequence: a workgroup for each block of 32 rows, of as many wavefronts as LDS has room for with three tiles of 32 keys each, in one launch
-// (attn_paged_few.hip).  Where a wavefront has up to 6 tiles, or up to 12 and the workgroups are not so few that most of the device would idle, and up to 512 workgroups: more of them take turns on a
+// With a window and one new token a sequence: a workgroup for each block of 32 rows, of wavefronts with three tiles of 32 keys of K and of V each, in one launch
+// (attn_paged_few.hip): as many as LDS has room for at d >= 64, eight (of thirteen) at d <= 32.  Where a wavefront has up to 6 tiles, one more where the window's edges and the last sink cut some, or up to 12 and the workgroups are not so few that most of the device would idle, and up to 512 workgroups: more of them take turns on a
 // compute unit, and a division by keys is evener.  us, divided with the join | this, sequences x K heads (workgroups), window.  d = 64: 1 x 2, 512 (3 tiles) 9.9 | 7.0, 1024 10.1 | 9.9, 2048 (11) 10.8 | 15.2;
 // 64 x 2, 512 14.0 | 7.9, 2048 23.1 | 17.3; 256 x 2, 512 27.6 | 19.3, 2048 59 | 50; 1024 x 2, 512 80 | 67.  d = 128: 1 x 8, 256 (3) 13.7 | 9.9, 512 (6) 13.8 | 13.2, 1024 (11) 14.5 | 21.0; 16 x 8, 256 14.3 |
 // 10.6, 1024 22.4 | 22.3; 33 x 8, 512 26.5 | 27.5; 64 x 8, 256 27.4 | 24.7, 512 35.6 | 33.0; 128 x 8, 512 58 | 62; 256 x 8, 256 71 | 83.  d = 32: 1 x 12, 2048 (8) 11.6 | 12.1; 20 x 12, 512 15.0 | 7.3, 2048 24.4 |

@@ -21,8 +21,9 @@ inline bool window_hides(int N, int window, int sinks) { return (int64_t)window 
 constexpr int window_query_tile(int d) { return d == 128 ? 32 : 64; }
 constexpr size_t window_piece_floats(int d) { return (size_t)2 * 32 * (d <= 32 ? 32 : d); }
 // How the gradients of the sinks are made.  Blocks of keys that hold sinks are swept by the queries behind the window too where that takes no longer than the launch: they come first, two
-// workgroups to a compute unit.  Else those queries are divided in stretches, which four wavefronts each take the tiles of in turn: about 128 in all, of at least 16 tiles, and of no more than
-// the other blocks of keys leave time for (a stretch's tile takes a quarter of twice as long as theirs).
+// workgroups to a compute unit.  Else those queries are divided in stretches, which four wavefronts each take the tiles of in turn: about 128 in all where heads and sinks are few, of at least 16 tiles, and of no more than
+// the other blocks of keys leave time for (a stretch's tile takes a quarter of twice as long as theirs).  There is one at least for every head and 32 sinks, so that with many sinks
+// time and workspace grow with them: stretches, us of the backward pass and MB, 16 x 16384, d = 128, window 1024, 4 | 256 | 1024 sinks 128, 520, 6.8 | 256, 620, 14.7 | 1024, 930, 52; window 128, 8000 sinks 4000, 2840, 264.
 // us of the backward pass with four sinks, stretches of 32 tiles | swept through, heads x N, window, tiles behind it, tiles of the launch's longest unit: d = 64 16 x 1024, 256, 12 of 2 25.6 | 38.3;
 // 128 x 1024, 256, 12 of 12 82.0 | 80.2; 64 x 2048, 256, 28 of 12 78.2 | 97.3; 300 x 300, 150, 3 of 7 56.5 | 50.9; d = 128 16 x 4096, 1024, 96 of 36 135 | 223; 210 x 333, 200, 5 of 12 85.8 | 70.6;
 // 64 x 16384, 1024, 480 of 576 2053 | 2040; 1 x 16384, 1024, 480 of 9 154 | 600.  Stretches of 16 | 32 | 64: d = 64 4 x 2048, 128 22.4 | 28.1 | 27.9; d = 32 8 x 8192, 100 28.1 | 30.1 | 39.8,

@@ -8,6 +8,7 @@
 //   One MI355X, bf16, operations of the visible pairs: 16 heads x 16384, d = 128, window 1024 and four sinks forward 175 us (765 TFLOP/s; 19 tiles are swept for 16 of pairs: 930 of what is executed), dQ 235 (855); the
 // matrix and vector units bound it, matrix units busy in 41 and 47 per cent of the cycles.  128 heads x 1024, d = 64, window 256: 26 and 40 us: a block has 7 tiles, and what it waits for at its start and its end, and 16
 // exponentials a lane to an MFMA, are most of it; HBM bytes (67 and 102 MB) take 12 and 19.
+//   With dropout (of probability 0.1) forward and backward pass take 206 and 612 us instead of 174 and 520, and 34 and 93 instead of 26 and 76; 5 x 12 x 1000, d = 32, window 300, padded, 15.3 and 41 instead of 13.0 and 30.
 #include "attn_window.h"
 
 #include "attn_tiles.h"
@@ -470,7 +471,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void window_dq_kernel(const Window
 }
 
 // The division of the forward and of dQ among wavefronts: with few blocks of rows, half as many rows to a block and two groups of wavefronts that take every other tile.
-// us, {4, 1} | {2, 2} (wavefronts of rows, groups), heads x N, window: forward d = 64 12 x 197, 64 7.2 | 5.1, 16 x 1024, 256 11.1 | 8.0, 8 x 4096, 512 15.8 | 12.9, 32 x 1024, 256 11.5 | 10.1,
+// us of calls in a replayed graph, without sinks, {4, 1} | {2, 2} (wavefronts of rows, groups), heads x N, window: forward d = 64 12 x 197, 64 7.2 | 5.1, 16 x 1024, 256 11.1 | 8.0, 8 x 4096, 512 15.8 | 12.9, 32 x 1024, 256 11.5 | 10.1,
 // 48 x 1024, 256 15.1 | 15.7, 16 x 4096, 512 21.1 | 23.4; d = 128 1 x 16384, 1024 28.7 | 22.6, 16 x 1024, 256 13.9 | 11.7, 32 x 1024, 256 14.8 | 22.0; d = 32 60 x 1000, 300 14.4 | 11.8.
 // Backward (dQ alone so): d = 64 8 x 4096, 512 35.2 | 33.3, 32 x 1024, 256 27.4 | 26.8, 48 x 1024, 256 35.9 | 38.9; d = 128 1 x 16384, 1024 142 | 134, 4 x 8192, 1024 112 | 122; d = 32 30 x 1000, 300
 // 23.5 | 20.9, 60 x 1000, 300 30.2 | 31.7.
@@ -478,7 +479,7 @@ bool window_divided(const WindowArgs& a, int64_t compute_units_blocks) {
   const int64_t blocks64 = (int64_t)a.k.B * a.k.H * ((a.k.N + 63) / 64);
   return blocks64 <= compute_units_blocks * kComputeUnits;
 }
-// (d = 64 in 128 registers, four workgroups to a compute unit instead of three, where there are more blocks than three to each; with dropout that spills.  us, heads x N, window, blocks, three | four:
+// (d = 64 in 128 registers, four workgroups to a compute unit instead of three, where there are more blocks than three to each: two of them go through scratch memory, 12 bytes a lane, and it is faster all the same; with dropout, which needs more, it stays at three.  us, heads x N, window, blocks, three | four:
 // 97 x 1024, 256, 776 25.8 | 22.7, 128 x 1024, 1024 28.5 | 26.4, 32 x 4096, 512, 1024 40.0 | 35.5, 128 x 2048, 1024, 2048 87.3 | 86.8, 300 x 1024, 128, 2400 42.8 | 40.8; 96 x 512, 100, 384 12.6 | 13.4, 64 x
 // 1024, 256, 512 16.4 | 16.9.)
 template <typename T, int D, int RW, int KG> int launch_fwd(WindowArgs a, bool dropout, hipStream_t s) {

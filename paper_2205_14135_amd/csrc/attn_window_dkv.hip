@@ -12,6 +12,7 @@
 // 128 heads x 1024, d = 64, window 256, swept through, 40 us.
 // P and dS are rounded to 16 bits, half a step each, for their products with dO and Q, as in the dense kernels: dK and dV are no further off than dQ (attn_window.hip).
 // Vector registers: d = 128 keeps the V rows in LDS (as there) and 32 queries to a tile, d <= 64 both operands in registers and 64 queries.
+// (At d = 128 four registers go through scratch memory, 20 bytes a lane.)
 #include "attn_window.h"
 
 #include <type_traits>
